@@ -259,6 +259,119 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
                    const float *lse_dec, float scale, int first, float *eigenvalues, float *z_vec,
                    float *gram, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Decay mixer: causal linear attention with a decay for each head, the mixer's counterpart for sequences that are read
+ * and written in order (linear in N too, with a state of fixed size instead of latents).  Per (b,h), with
+ * l = exp(log_decay[h]):
+ *     S_t = l S_{t-1} + k_t v_t^T   (d x d, S_{-1} = state_in or 0),      o_t = scale * S_t^T q_t
+ * flare_decay_forward takes whole sequences (training; prompts, whose state it returns), flare_decay_step one token of
+ * each item.  Everything said under "Conventions" above holds (contiguous, 16-byte aligned, on `stream`, nothing
+ * allocated, the same bits in every run), with these shapes and types:
+ *   - B,H,N >= 1 with B*H <= 65535, N < 2^24 and N times the token stride below 2^32; d in {16, 32, 64, 128}; dtype f32,
+ *     bf16 or f16; token tensors q, k, v, o, d_o, dq, dk, dv [B][H][N][d] or [B][N][H][d].
+ *   - log_decay [H] fp32, natural logarithms, at most 0 (0: no decay).  It is not differentiated.  A head whose log decay
+ *     is above 0 or NaN gets NaN outputs.
+ *   - lengths [B] int32 on the device, or NULL (every item has N tokens): a padded batch.  Item b has lengths[b] tokens
+ *     (taken as 0 below 0 and as N above N); rows behind them are not read, and those of the outputs are written as zeros.
+ *     The state goes by the item's own tokens; with none it is handed on unchanged.
+ *   - states and their gradients are [B][H][d][d] fp32, rows by q and k, columns by v.
+ * 16-bit storage: products of the stored values are exact and sums fp32; <q,k> with its weight, and the state where it
+ * meets q, are rounded to the storage type (fp16 behind a common power of two); what is added to the state is not
+ * rounded (weights times v to 2^-22 of a term).  f32 storage runs on the fp32 matrix instructions.
+ * With f16 storage scale times q, k, v and d_o must stay below 65504 in magnitude.
+ */
+typedef struct {
+    int B, H, N, d;
+    flare_dtype dtype;
+    flare_layout layout;
+} flare_decay_shape;
+
+/* Scratch bytes of flare_decay_forward and flare_decay_backward (either pointer may be NULL); may be 0.  Host-only. */
+int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes);
+
+/*
+ *   q, k, v, log_decay, lengths (or NULL), state_in (or NULL: zero)                                       (in)
+ *   o: q's shape and dtype; state_out (or NULL)                                                           (out)
+ * o may be the buffer of q, k or v, and state_out that of state_in.
+ */
+int flare_decay_forward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                        const int *lengths, const float *state_in, void *o, float *state_out, float scale,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Backward.  With G_t the gradient of S_{t-1} (G behind the last token = dstate_out, or zero):
+ *     dS_t = scale q_t d_o_t^T + G_{t+1},  G_t = l dS_t,  dq_t = scale S_t d_o_t,  dk_t = dS_t v_t,  dv_t = dS_t^T k_t
+ *   q, k, v, log_decay, lengths, state_in as in the forward; d_o: o's gradient; dstate_out (or NULL: zero)  (in)
+ *   dq, dk, dv: q's shape and dtype; dstate_in (or NULL)                                                  (out)
+ * No output may overlap an input.
+ */
+int flare_decay_backward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                         const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq,
+                         void *dk, void *dv, float *dstate_in, float scale, void *workspace, size_t workspace_bytes,
+                         void *stream);
+
+/*
+ * One token of each item: shape->N is 1 (else FLARE_EINVAL); q, k, v, o are [B][H][d].
+ *   active [B] int32 or NULL: an item with active[b] <= 0 has no token now: its state is handed on, its o is zero  (in)
+ *   state_in, state_out: may be one buffer                                                            (in, out)
+ */
+int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                     const int *active, const float *state_in, float *state_out, void *o, float scale, void *stream);
+
+/*
+ * Residual norm: what stands around a block's branch (the pre-norm residual of Appendix B.1, X += branch(LN(X)), and its
+ * variants) in one pass over each token's channels.  Per row of C channels
+ *     u = post(y),   a = u * act(gate),   x_out = x + alpha * a,   h = pre(x_out)
+ * post: the norm of the branch's output y; pre: the norm that the next branch starts with.  Both are a layer norm
+ * ((t - mean) / sqrt(var + eps) * weight + bias), an RMS norm (t / sqrt(mean t^2 + eps) * weight [+ bias]) or none.
+ * gate: a row for each rows_per_gate rows of x (1: one for each token; N: one for each item of N tokens; rows: one for
+ * all, a learned scale of the channels).
+ *   - rows >= 1, 1 <= C <= 8192, all tensors [rows][C] and contiguous (the gate [rows / rows_per_gate][C], a whole number).
+ *     y, gate and h have the type dtype; x and x_out too, or fp32 with x_f32 (a residual stream in fp32 beside 16-bit
+ *     branches).  Weights and biases are [C] fp32 or NULL (1 and 0).
+ *   - y may be NULL (before the first block): then post and gate are none, and x_out is not written (pass NULL).
+ *     pre none: h is not written (pass NULL).
+ *   - All arithmetic is fp32; h is formed from x_out before that is rounded.  Outputs are rounded once.
+ *   - x_out may be the buffer of x or y, h that of y (not the same as x_out's); dx that of dx_out, dy that of dh or y.
+ */
+typedef enum { FLARE_NORM_NONE = 0, FLARE_NORM_LAYER = 1, FLARE_NORM_RMS = 2 } flare_norm;
+typedef enum {
+    FLARE_GATE_NONE = 0,
+    FLARE_GATE_PLAIN = 1,      /* act(g) = g */
+    FLARE_GATE_SIGMOID = 2,    /* 1 / (1 + exp(-g)) */
+    FLARE_GATE_SILU = 3        /* g / (1 + exp(-g)) */
+} flare_gate;
+typedef struct {
+    long long rows;
+    int C;
+    flare_dtype dtype;
+    int x_f32;
+    flare_norm pre, post;
+    flare_gate gate;
+    long long rows_per_gate;   /* ignored without a gate */
+} flare_norm_shape;
+typedef struct {
+    const float *pre_weight, *pre_bias, *post_weight, *post_bias;
+} flare_norm_params;
+
+/* Scratch bytes of flare_residual_norm_backward.  Host-only. */
+int flare_residual_norm_workspace_bytes(const flare_norm_shape *shape, size_t *bytes);
+
+/* stats [rows][4] fp32, kept for the backward, or NULL: mean and 1/sqrt(var + eps) of pre, then of post (what belongs to
+ * a norm that is none stays as it was).  params may be NULL (no weights, no biases). */
+int flare_residual_norm_forward(const flare_norm_shape *shape, const flare_norm_params *params, const void *x, const void *y,
+                                const void *gate, void *x_out, void *h, float *stats, float alpha, float eps, void *stream);
+
+/*
+ *   x, y, gate, params, stats as in the forward; dx_out, dh: the gradients of x_out and h, either may be NULL (zero)  (in)
+ *   dx, dy, dgate in the types of x, y and gate; the gradients of weights and biases [C] fp32                      (out)
+ * Each output may be NULL (not wanted).  dgate of a gate that several rows share is summed over them in fp32.
+ */
+int flare_residual_norm_backward(const flare_norm_shape *shape, const flare_norm_params *params, const void *x, const void *y,
+                                 const void *gate, const float *stats, const void *dx_out, const void *dh, void *dx, void *dy,
+                                 void *dgate, float *dpre_weight, float *dpre_bias, float *dpost_weight, float *dpost_bias,
+                                 float alpha, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

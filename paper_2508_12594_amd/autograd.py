@@ -1,4 +1,5 @@
-"""torch.autograd wrapper around the binding: `flare_mixer(q_lat, k, v, scale)` is differentiable.
+"""torch.autograd wrappers around the binding: `flare_mixer(q_lat, k, v, scale)`, `decay_mixer(q, k, v, log_decay, scale)`
+and `residual_norm(x, y)` are differentiable.
 
 Nothing is computed here: the forward calls flare_forward (keeping z, lse_enc, lse_dec and y for the
 backward), the backward calls flare_backward_cast (dq_lat in q_lat's dtype, which autograd requires of a
@@ -48,3 +49,99 @@ def flare_mixer(q_lat, k, v, scale, layout="bhnd", y_f32=False):
     if y is None:
         y = _recorded().apply(q_lat, k, v, float(scale), layout, bool(y_f32))
     return y
+
+
+_RECORDED_DECAY = None
+
+
+def _recorded_decay():
+    global _RECORDED_DECAY
+    if _RECORDED_DECAY is None:
+        import torch
+
+        class RecordedDecayMixer(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, v, log_decay, lengths, state, scale, want_state, layout):
+                whole = lambda t: None if t is None else t.contiguous()   # noqa: E731
+                q, k, v, log_decay, lengths, state = (whole(t) for t in (q, k, v, log_decay, lengths, state))
+                o, state_out = binding.decay_forward(q, k, v, log_decay, scale, lengths=lengths, state=state,
+                                                     want_state=want_state, layout=layout)
+                ctx.save_for_backward(q, k, v, log_decay, lengths, state)
+                ctx.scale, ctx.layout = scale, layout
+                return (o, state_out) if want_state else o
+
+            @staticmethod
+            def backward(ctx, d_o, dstate_out=None):
+                q, k, v, log_decay, lengths, state = ctx.saved_tensors
+                dq, dk, dv, dstate = binding.decay_backward(
+                    q, k, v, log_decay, d_o.contiguous(), ctx.scale, lengths=lengths, state=state,
+                    dstate_out=None if dstate_out is None else dstate_out.contiguous(),
+                    want_dstate=state is not None and ctx.needs_input_grad[5], layout=ctx.layout)
+                return dq, dk, dv, None, None, dstate, None, None, None
+
+        _RECORDED_DECAY = RecordedDecayMixer
+    return _RECORDED_DECAY
+
+
+def decay_mixer(q, k, v, log_decay, scale, lengths=None, state=None, want_state=False, layout="bhnd"):
+    """Causal linear attention with a decay for each head (flare_decay_forward): per head S_t = exp(log_decay) S_{t-1} + k_t v_t^T,
+    o_t = scale S_t^T q_t.  q, k, v [B,H,N,d] ('bhnd') or [B,N,H,d] ('bnhd'), log_decay [H] fp32 and at most 0 (a constant: it is
+    not differentiated), lengths [B] int32 for a padded batch, state [B,H,d,d] fp32 from an earlier piece of the
+    sequences.  Returns (o, state_out), state_out None without want_state.  Differentiable in q, k, v and state."""
+    out = binding._native().decay_mixer(q, k, v, log_decay, float(scale), lengths, state, bool(want_state),
+                                        binding._layout(layout))
+    if out is None:
+        if log_decay.requires_grad:
+            raise binding.FlareError("log_decay is not differentiated: pass it detached")
+        out = _recorded_decay().apply(q, k, v, log_decay, lengths, state, float(scale), bool(want_state), layout)
+        out = out if want_state else (out, None)
+    return out
+
+
+_RECORDED_NORM = None
+
+
+def _recorded_norm():
+    global _RECORDED_NORM
+    if _RECORDED_NORM is None:
+        import torch
+
+        class RecordedResidualNorm(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x, y, gate, pre_weight, pre_bias, post_weight, post_bias, kinds, eps, h_dtype):
+                whole = lambda t: None if t is None else t.contiguous()   # noqa: E731
+                tensors = [whole(t) for t in (x, y, gate, pre_weight, pre_bias, post_weight, post_bias)]
+                stats = torch.empty((tensors[0].numel() // tensors[0].shape[-1], 4), dtype=torch.float32, device=x.device)
+                names = ("pre_weight", "pre_bias", "post_weight", "post_bias")
+                x_out, h = binding.residual_norm_forward(*tensors[:3], **dict(zip(names, tensors[3:])), **kinds, eps=eps,
+                                                         stats=stats, h_dtype=h_dtype)
+                ctx.save_for_backward(stats, *tensors)
+                ctx.kinds, ctx.outputs = kinds, (x_out is not None, h is not None)
+                return (x_out, h) if all(ctx.outputs) else h if x_out is None else x_out
+
+            @staticmethod
+            def backward(ctx, *grads):
+                grads = [g if g is None else g.contiguous() for g in grads]
+                dx_out = grads.pop(0) if ctx.outputs[0] else None
+                dh = grads.pop(0) if ctx.outputs[1] else None
+                stats, x, y, gate, *params = ctx.saved_tensors
+                names = ("pre_weight", "pre_bias", "post_weight", "post_bias")
+                return binding.residual_norm_backward(x, y, dx_out, dh, stats, gate=gate, **dict(zip(names, params)),
+                                                      **ctx.kinds) + (None, None, None)
+
+        _RECORDED_NORM = RecordedResidualNorm
+    return _RECORDED_NORM
+
+
+def residual_norm(x, y=None, gate=None, pre="layer", post="none", pre_weight=None, pre_bias=None, post_weight=None, post_bias=None,
+                  gate_act="none", alpha=1.0, eps=1e-5, h_dtype=None):
+    """x_out = x + alpha * post(y) * gate_act(gate) and h = pre(x_out) in one pass (flare_residual_norm_forward; shapes as in
+    binding.residual_norm_forward).  Returns (x_out, h): without y x_out is x, with pre 'none' h is None.  Differentiable in
+    all tensors."""
+    kinds = dict(pre=pre, post=post, gate_act=gate_act, alpha=float(alpha))
+    out = binding._native().residual_norm(x, y, gate, binding._norm(pre, "pre"), binding._norm(post, "post"), binding._gate(gate_act),
+                                          pre_weight, pre_bias, post_weight, post_bias, float(alpha), float(eps), h_dtype)
+    if out is None:
+        made = _recorded_norm().apply(x, y, gate, pre_weight, pre_bias, post_weight, post_bias, kinds, float(eps), h_dtype)
+        out = made if y is not None and pre != "none" else (None, made) if y is None else (made, None)
+    return (x if y is None else out[0]), out[1]

@@ -25,13 +25,31 @@ EXPORTS = [
     "flare_forward", "flare_forward_static", "flare_decode_project", "flare_forward_project", "flare_backward",
     "flare_backward_cast", "flare_profile_enable", "flare_profile_kernels",
     "flare_profile_name", "flare_profile_read", "flare_spectral_workspace_bytes", "flare_spectral",
+    "flare_decay_workspace_bytes", "flare_decay_forward", "flare_decay_backward", "flare_decay_step",
+    "flare_residual_norm_workspace_bytes", "flare_residual_norm_forward", "flare_residual_norm_backward",
 ]
+NORMS = {"none": 0, "layer": 1, "rms": 2}                # flare_norm
+GATES = {"none": 1, "sigmoid": 2, "silu": 3}             # flare_gate: what a gate goes through
 
 
 class FlareShape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("N", ctypes.c_int), ("M", ctypes.c_int),
                 ("d", ctypes.c_int), ("dtype", ctypes.c_int), ("layout", ctypes.c_int),
                 ("shared_latents", ctypes.c_int), ("y_f32", ctypes.c_int), ("variant", ctypes.c_int)]
+
+
+class DecayShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("N", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("layout", ctypes.c_int)]
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong), ("C", ctypes.c_int), ("dtype", ctypes.c_int), ("x_f32", ctypes.c_int),
+                ("pre", ctypes.c_int), ("post", ctypes.c_int), ("gate", ctypes.c_int), ("rows_per_gate", ctypes.c_longlong)]
+
+
+class NormParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pre_weight", "pre_bias", "post_weight", "post_bias")]
 
 
 class FlareError(RuntimeError):
@@ -70,12 +88,24 @@ def load():
     lib.flare_backward_cast.argtypes = lib.flare_backward.argtypes
     lib.flare_spectral_workspace_bytes.argtypes = [sp, ctypes.POINTER(ctypes.c_size_t)]
     lib.flare_spectral.argtypes = [sp, vp, vp, fp, fp, ctypes.c_float, ctypes.c_int, fp, fp, fp, vp, ctypes.c_size_t, vp]
+    size, dp, np = ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(DecayShape), ctypes.POINTER(NormShape)
+    pp, f = ctypes.POINTER(NormParams), ctypes.c_float
+    lib.flare_decay_workspace_bytes.argtypes = [dp, size, size]
+    lib.flare_decay_forward.argtypes = [dp, vp, vp, vp, fp, vp, fp, vp, fp, f, vp, ctypes.c_size_t, vp]
+    lib.flare_decay_backward.argtypes = [dp, vp, vp, vp, fp, vp, fp, vp, fp, vp, vp, vp, fp, f, vp, ctypes.c_size_t, vp]
+    lib.flare_decay_step.argtypes = [dp, vp, vp, vp, fp, vp, fp, fp, vp, f, vp]
+    lib.flare_residual_norm_workspace_bytes.argtypes = [np, size]
+    lib.flare_residual_norm_forward.argtypes = [np, pp, vp, vp, vp, vp, vp, fp, f, f, vp]
+    lib.flare_residual_norm_backward.argtypes = [np, pp, vp, vp, vp, fp, vp, vp, vp, vp, vp, fp, fp, fp, fp, f, vp,
+                                                 ctypes.c_size_t, vp]
     lib.flare_profile_enable.argtypes = [ctypes.c_int]
     lib.flare_profile_name.restype = ctypes.c_char_p
     lib.flare_profile_name.argtypes = [ctypes.c_int]
     lib.flare_profile_read.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int)]
     for name in ("flare_spectral_workspace_bytes", "flare_spectral", "flare_workspace_bytes", "flare_encode", "flare_decode", "flare_forward", "flare_backward",
-                 "flare_backward_cast", "flare_profile_enable", "flare_profile_kernels", "flare_profile_read"):
+                 "flare_backward_cast", "flare_profile_enable", "flare_profile_kernels", "flare_profile_read",
+                 "flare_decay_workspace_bytes", "flare_decay_forward", "flare_decay_backward", "flare_decay_step",
+                 "flare_residual_norm_workspace_bytes", "flare_residual_norm_forward", "flare_residual_norm_backward"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -252,6 +282,78 @@ def spectral(q_lat, k, lse_enc, lse_dec, scale, first=0, want_gram=False, stream
                                  ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()), _stream(stream)),
            "flare_spectral")
     return ev, zv, gram
+
+
+# ---- decay mixer -----------------------------------------------------------------------------------------------------
+def decay_workspace_bytes(B, H, N, d, dtype_code, layout="bhnd"):
+    """(forward bytes, backward bytes) of scratch of the decay mixer for this shape; may be 0."""
+    shp = DecayShape(B, H, N, d, dtype_code, _layout(layout))
+    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(load().flare_decay_workspace_bytes(ctypes.byref(shp), ctypes.byref(f), ctypes.byref(b)),
+           "flare_decay_workspace_bytes")
+    return int(f.value), int(b.value)
+
+
+def decay_forward(q, k, v, log_decay, scale, lengths=None, state=None, o=None, state_out=None, want_state=False,
+                  workspace=None, stream=None, layout="bhnd"):
+    """flare_decay_forward: causal linear attention with a decay for each head; returns (o, state_out).
+
+    layout 'bhnd': q, k, v, o are [B,H,N,d]; 'bnhd': they are [B,N,H,d].  log_decay [H] fp32, at most 0.  lengths [B] int32:
+    a padded batch.  state [B,H,d,d] fp32: what came before the first token.  state_out is written where it is given
+    (it may be `state`) or with want_state, and None otherwise."""
+    return (_ext or _native()).decay_forward(q, k, v, log_decay, scale, lengths, state, o, state_out, bool(want_state),
+                                             workspace, stream, _layout(layout))
+
+
+def decay_backward(q, k, v, log_decay, d_o, scale, lengths=None, state=None, dstate_out=None, dq=None, dk=None, dv=None,
+                   dstate=None, want_dstate=False, workspace=None, stream=None, layout="bhnd"):
+    """flare_decay_backward: returns (dq, dk, dv, dstate); dstate, the gradient of `state`, is written where it is given or
+    with want_dstate, and None otherwise.  dstate_out: the gradient of the forward's state_out."""
+    return (_ext or _native()).decay_backward(q, k, v, log_decay, d_o, scale, lengths, state, dstate_out, dq, dk, dv, dstate,
+                                              bool(want_dstate), workspace, stream, _layout(layout))
+
+
+def decay_step(q, k, v, log_decay, state, scale, state_out=None, active=None, o=None, stream=None):
+    """flare_decay_step: one token of each item, q, k, v [B,H,d]; returns o [B,H,d].  state [B,H,d,d] fp32 is advanced in
+    place, or into state_out.  active [B] int32: items with 0 are left out (their state stays, their o is zero)."""
+    return (_ext or _native()).decay_step(q, k, v, log_decay, state, scale, state_out, active, o, stream)
+
+
+# ---- residual norm -----------------------------------------------------------------------------------------------------
+def _norm(kind, what):
+    try:
+        return NORMS[kind]
+    except (KeyError, TypeError):
+        raise FlareError("%s must be 'none', 'layer' or 'rms'" % what) from None
+
+
+def _gate(act):
+    try:
+        return GATES[act]
+    except (KeyError, TypeError):
+        raise FlareError("gate_act must be 'none', 'sigmoid' or 'silu'") from None
+
+
+def residual_norm_forward(x, y=None, gate=None, pre="layer", post="none", pre_weight=None, pre_bias=None, post_weight=None,
+                          post_bias=None, gate_act="none", alpha=1.0, eps=1e-5, x_out=None, h=None, stats=None, h_dtype=None,
+                          stream=None):
+    """flare_residual_norm_forward: x_out = x + alpha * post(y) * gate_act(gate), h = pre(x_out); returns (x_out, h).
+
+    x, y [..., C]; gate: x's shape, that shape with ones where rows share it ([B,1,C] beside [B,N,C]), or [C]; weights and
+    biases [C] fp32.  x may be fp32 beside a 16-bit y.  Without y (before the first block) x_out is None and h = pre(x), in
+    h_dtype if given; with pre 'none' h is None.  stats [rows,4] fp32 is filled when given (for the backward)."""
+    return (_ext or _native()).residual_norm_forward(x, y, gate, _norm(pre, "pre"), _norm(post, "post"), _gate(gate_act), pre_weight,
+                                                     pre_bias, post_weight, post_bias, alpha, eps, x_out, h, stats, h_dtype,
+                                                     stream)
+
+
+def residual_norm_backward(x, y, dx_out, dh, stats, gate=None, pre="layer", post="none", pre_weight=None, pre_bias=None,
+                           post_weight=None, post_bias=None, gate_act="none", alpha=1.0, workspace=None, stream=None):
+    """flare_residual_norm_backward: the gradients of (x, y, gate, pre_weight, pre_bias, post_weight, post_bias), None for
+    what was not given.  x, y, gate and stats are the forward's; dx_out and dh may be None (zero)."""
+    return tuple((_ext or _native()).residual_norm_backward(x, y, dx_out, dh, stats, gate, _norm(pre, "pre"), _norm(post, "post"),
+                                                            _gate(gate_act), pre_weight, pre_bias, post_weight, post_bias, alpha,
+                                                            workspace, stream))
 
 
 def profile_enable(on):

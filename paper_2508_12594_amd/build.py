@@ -26,7 +26,7 @@ RATES_SOURCES = {"machine_rates.hip": []}
 SOURCES = {"flare_api.hip": [], "flare_valu.hip": [], "flare_mfma_f32.hip": ["-fno-honor-nans"],
            "flare_mfma_fwd.hip": ["-fno-honor-nans"],
            "flare_mfma_bwd.hip": ["-fno-honor-nans"], "flare_mfma_proj.hip": ["-fno-honor-nans"],
-           "flare_spectral.hip": []}
+           "flare_spectral.hip": [], "flare_decay.hip": [], "flare_norm.hip": []}
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

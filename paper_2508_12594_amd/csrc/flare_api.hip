@@ -41,7 +41,8 @@ const char *const kKernelNames[KID_COUNT] = {
     "encode_partial", "encode_merge", "decode", "bwd_token_stats", "bwd_prep", "bwd_dz_partial",
     "bwd_dz_merge", "bwd_dq_partial", "bwd_dq_reduce", "bwd_dkdv",
     "decode_merge", "spectral_gram", "spectral_reduce", "spectral_eigen",
-    "spectral_post", "decode_project"};
+    "spectral_post", "decode_project", "decay_sum", "decay_carry", "decay_forward", "decay_backward", "decay_step",
+    "norm_forward", "norm_backward", "norm_sum"};
 }  // namespace
 
 LaunchTimer::LaunchTimer(int kid, hipStream_t s) : slot(-1), stream(s)
@@ -96,6 +97,49 @@ int check_shape(const flare_shape *s)
     return FLARE_OK;
 }
 
+int check_decay(const flare_decay_shape *s)
+{
+    if (!s) return FLARE_EINVAL;
+    if (s->B < 1 || s->H < 1 || s->N < 1 || s->d < 1) return FLARE_EINVAL;
+    if (s->dtype != FLARE_F32 && s->dtype != FLARE_BF16 && s->dtype != FLARE_F16) return FLARE_EUNSUPPORTED;
+    if (s->layout != FLARE_BHND && s->layout != FLARE_BNHD) return FLARE_EUNSUPPORTED;
+    if (s->d != 16 && s->d != 32 && s->d != 64 && s->d != 128) return FLARE_EUNSUPPORTED;
+    if ((long long)s->B * s->H > 65535) return FLARE_EUNSUPPORTED;
+    const long long sn = (s->layout == FLARE_BNHD) ? (long long)s->H * s->d : s->d;   // as in check_shape
+    if (s->N >= (1 << 24) || sn >= (1 << 24) || (long long)s->N * sn >= (1LL << 32)) return FLARE_EUNSUPPORTED;
+    return FLARE_OK;
+}
+
+int check_norm(const flare_norm_shape *s)
+{
+    if (!s) return FLARE_EINVAL;
+    if (s->rows < 1 || s->C < 1) return FLARE_EINVAL;
+    if (s->dtype != FLARE_F32 && s->dtype != FLARE_BF16 && s->dtype != FLARE_F16) return FLARE_EUNSUPPORTED;
+    if (s->x_f32 != 0 && s->x_f32 != 1) return FLARE_EINVAL;
+    if (s->pre < FLARE_NORM_NONE || s->pre > FLARE_NORM_RMS || s->post < FLARE_NORM_NONE || s->post > FLARE_NORM_RMS ||
+        s->gate < FLARE_GATE_NONE || s->gate > FLARE_GATE_SILU)
+        return FLARE_EINVAL;
+    if (s->gate != FLARE_GATE_NONE && (s->rows_per_gate < 1 || s->rows % s->rows_per_gate != 0)) return FLARE_EINVAL;
+    if (s->C > 8192 || s->rows >= (1LL << 31)) return FLARE_EUNSUPPORTED;
+    return FLARE_OK;
+}
+
+// What both directions of the residual norm ask of their inputs.
+int check_norm_inputs(const flare_norm_shape *s, const flare_norm_params *p, const void *x, const void *y, const void *gate)
+{
+    const int rc = check_norm(s);
+    if (rc != FLARE_OK) return rc;
+    if (!x) return FLARE_EINVAL;
+    if (!y && (s->post != FLARE_NORM_NONE || s->gate != FLARE_GATE_NONE || s->pre == FLARE_NORM_NONE)) return FLARE_EINVAL;
+    if ((gate != nullptr) != (s->gate != FLARE_GATE_NONE)) return FLARE_EINVAL;
+    if (p && s->pre == FLARE_NORM_NONE && (p->pre_weight || p->pre_bias)) return FLARE_EINVAL;
+    if (p && s->post == FLARE_NORM_NONE && (p->post_weight || p->post_bias)) return FLARE_EINVAL;
+    if (!aligned16(x) || !aligned16(y) || !aligned16(gate) ||
+        (p && (!aligned16(p->pre_weight) || !aligned16(p->pre_bias) || !aligned16(p->post_weight) || !aligned16(p->post_bias))))
+        return FLARE_EALIGN;
+    return FLARE_OK;
+}
+
 }  // namespace
 }  // namespace flare
 
@@ -103,7 +147,7 @@ using namespace flare;
 
 extern "C" {
 
-int flare_version(void) { return 500; }   // 0.5.0: flare_backward_cast
+int flare_version(void) { return 600; }   // 0.6.0: flare_decay_*, flare_residual_norm_*
 
 const char *flare_strerror(int status)
 {
@@ -293,6 +337,99 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
     if (!workspace || workspace_bytes < spectral_bytes(*shape)) return FLARE_EWORKSPACE;
     return spectral_run(*shape, q_lat, k, lse_enc, lse_dec, scale, first, eigenvalues, z_vec, gram, workspace,
                         static_cast<hipStream_t>(stream));
+}
+
+int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes)
+{
+    const int rc = check_decay(shape);
+    if (rc != FLARE_OK) return rc;
+    if (fwd_bytes) *fwd_bytes = decay_fwd_bytes(*shape);
+    if (bwd_bytes) *bwd_bytes = decay_bwd_bytes(*shape);
+    return FLARE_OK;
+}
+
+int flare_decay_forward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                        const int *lengths, const float *state_in, void *o, float *state_out, float scale, void *workspace,
+                        size_t workspace_bytes, void *stream)
+{
+    const int rc = check_decay(shape);
+    if (rc != FLARE_OK) return rc;
+    if (!q || !k || !v || !log_decay || !o) return FLARE_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(lengths) ||
+        !aligned16(state_in) || !aligned16(o) || !aligned16(state_out) || !aligned16(workspace))
+        return FLARE_EALIGN;
+    const size_t need = decay_fwd_bytes(*shape);
+    if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
+    return decay_forward(*shape, q, k, v, log_decay, lengths, state_in, o, state_out, scale, workspace,
+                         static_cast<hipStream_t>(stream));
+}
+
+int flare_decay_backward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                         const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq, void *dk,
+                         void *dv, float *dstate_in, float scale, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_decay(shape);
+    if (rc != FLARE_OK) return rc;
+    if (!q || !k || !v || !log_decay || !d_o || !dq || !dk || !dv) return FLARE_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(lengths) ||
+        !aligned16(state_in) || !aligned16(d_o) || !aligned16(dstate_out) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
+        !aligned16(dstate_in) || !aligned16(workspace))
+        return FLARE_EALIGN;
+    const size_t need = decay_bwd_bytes(*shape);
+    if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
+    return decay_backward(*shape, q, k, v, log_decay, lengths, state_in, d_o, dstate_out, dq, dk, dv, dstate_in, scale, workspace,
+                          static_cast<hipStream_t>(stream));
+}
+
+int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                     const int *active, const float *state_in, float *state_out, void *o, float scale, void *stream)
+{
+    const int rc = check_decay(shape);
+    if (rc != FLARE_OK) return rc;
+    if (shape->N != 1 || !q || !k || !v || !log_decay || !state_in || !state_out || !o) return FLARE_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(active) || !aligned16(state_in) ||
+        !aligned16(state_out) || !aligned16(o))
+        return FLARE_EALIGN;
+    return decay_step(*shape, q, k, v, log_decay, active, state_in, state_out, o, scale, static_cast<hipStream_t>(stream));
+}
+
+int flare_residual_norm_workspace_bytes(const flare_norm_shape *shape, size_t *bytes)
+{
+    const int rc = check_norm(shape);
+    if (rc != FLARE_OK) return rc;
+    if (bytes) *bytes = norm_bwd_bytes(*shape);
+    return FLARE_OK;
+}
+
+int flare_residual_norm_forward(const flare_norm_shape *shape, const flare_norm_params *params, const void *x, const void *y,
+                                const void *gate, void *x_out, void *h, float *stats, float alpha, float eps, void *stream)
+{
+    const int rc = check_norm_inputs(shape, params, x, y, gate);
+    if (rc != FLARE_OK) return rc;
+    if ((x_out != nullptr) != (y != nullptr) || (h != nullptr) != (shape->pre != FLARE_NORM_NONE)) return FLARE_EINVAL;
+    if (!aligned16(x_out) || !aligned16(h) || !aligned16(stats)) return FLARE_EALIGN;
+    return norm_forward(*shape, params ? *params : flare_norm_params{}, x, y, gate, x_out, h, stats, alpha, eps,
+                        static_cast<hipStream_t>(stream));
+}
+
+int flare_residual_norm_backward(const flare_norm_shape *shape, const flare_norm_params *params, const void *x, const void *y,
+                                 const void *gate, const float *stats, const void *dx_out, const void *dh, void *dx, void *dy,
+                                 void *dgate, float *dpre_weight, float *dpre_bias, float *dpost_weight, float *dpost_bias,
+                                 float alpha, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_norm_inputs(shape, params, x, y, gate);
+    if (rc != FLARE_OK) return rc;
+    if (!stats && (shape->pre != FLARE_NORM_NONE || shape->post != FLARE_NORM_NONE)) return FLARE_EINVAL;
+    if ((!y && (dx_out || dy || dpost_weight || dpost_bias)) || (shape->gate == FLARE_GATE_NONE && dgate)) return FLARE_EINVAL;
+    if (shape->pre == FLARE_NORM_NONE && (dh || dpre_weight || dpre_bias)) return FLARE_EINVAL;
+    if (shape->post == FLARE_NORM_NONE && (dpost_weight || dpost_bias)) return FLARE_EINVAL;
+    if (!aligned16(stats) || !aligned16(dx_out) || !aligned16(dh) || !aligned16(dx) || !aligned16(dy) || !aligned16(dgate) ||
+        !aligned16(dpre_weight) || !aligned16(dpre_bias) || !aligned16(dpost_weight) || !aligned16(dpost_bias) ||
+        !aligned16(workspace))
+        return FLARE_EALIGN;
+    if (!workspace || workspace_bytes < norm_bwd_bytes(*shape)) return FLARE_EWORKSPACE;
+    return norm_backward(*shape, params ? *params : flare_norm_params{}, x, y, gate, stats, dx_out, dh, dx, dy, dgate, dpre_weight,
+                         dpre_bias, dpost_weight, dpost_bias, alpha, workspace, static_cast<hipStream_t>(stream));
 }
 
 int flare_profile_enable(int on)

@@ -30,6 +30,14 @@ enum KernelId {
     KID_SPECTRAL_EIGEN,
     KID_SPECTRAL_POST,
     KID_DECODE_PROJECT,
+    KID_DECAY_SUM,
+    KID_DECAY_CARRY,
+    KID_DECAY_FORWARD,
+    KID_DECAY_BACKWARD,
+    KID_DECAY_STEP,
+    KID_NORM_FORWARD,
+    KID_NORM_BACKWARD,
+    KID_NORM_SUM,
     KID_COUNT
 };
 
@@ -186,5 +194,25 @@ int mfma_gram_partial(const flare_shape &s, const Split &sp, const void *q, cons
 size_t spectral_bytes(const flare_shape &s);
 int spectral_run(const flare_shape &s, const void *q, const void *k, const float *lse_enc, const float *lse_dec,
                  float scale, int first, float *evals, float *zvec, float *gram, void *ws, hipStream_t stream);
+
+// ---- decay mixer (flare_decay.hip); state_in, lengths, state_out, dstate_* and active may be NULL ----------
+size_t decay_fwd_bytes(const flare_decay_shape &s);
+size_t decay_bwd_bytes(const flare_decay_shape &s);
+int decay_forward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
+                  const int *lengths, const float *state_in, void *o, float *state_out, float scale, void *ws,
+                  hipStream_t stream);
+int decay_backward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
+                   const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq, void *dk,
+                   void *dv, float *dstate_in, float scale, void *ws, hipStream_t stream);
+int decay_step(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay, const int *active,
+               const float *state_in, float *state_out, void *o, float scale, hipStream_t stream);
+
+// ---- residual norm (flare_norm.hip) --------------------------------------------------------------
+size_t norm_bwd_bytes(const flare_norm_shape &s);
+int norm_forward(const flare_norm_shape &s, const flare_norm_params &p, const void *x, const void *y, const void *gate, void *x_out,
+                 void *h, float *stats, float alpha, float eps, hipStream_t stream);
+int norm_backward(const flare_norm_shape &s, const flare_norm_params &p, const void *x, const void *y, const void *gate,
+                  const float *stats, const void *dx_out, const void *dh, void *dx, void *dy, void *dgate, float *dpre_weight,
+                  float *dpre_bias, float *dpost_weight, float *dpost_bias, float alpha, void *ws, hipStream_t stream);
 
 }  // namespace flare

@@ -14,9 +14,12 @@
 #include <ATen/ATen.h>
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
+#include <limits.h>
 
 #include <optional>
 #include <stdexcept>
@@ -46,6 +49,13 @@ struct Library {
     decltype(&flare_forward_project) forward_project = nullptr;
     decltype(&flare_backward) backward = nullptr;
     decltype(&flare_backward_cast) backward_cast = nullptr;
+    decltype(&flare_decay_workspace_bytes) decay_workspace_bytes = nullptr;
+    decltype(&flare_decay_forward) decay_forward = nullptr;
+    decltype(&flare_decay_backward) decay_backward = nullptr;
+    decltype(&flare_decay_step) decay_step = nullptr;
+    decltype(&flare_residual_norm_workspace_bytes) norm_workspace_bytes = nullptr;
+    decltype(&flare_residual_norm_forward) norm_forward = nullptr;
+    decltype(&flare_residual_norm_backward) norm_backward = nullptr;
 } lib;
 
 template <typename F>
@@ -68,6 +78,13 @@ void load_library(const std::string &path)
     resolve(h, "flare_forward_project", lib.forward_project);
     resolve(h, "flare_backward", lib.backward);
     resolve(h, "flare_backward_cast", lib.backward_cast);
+    resolve(h, "flare_decay_workspace_bytes", lib.decay_workspace_bytes);
+    resolve(h, "flare_decay_forward", lib.decay_forward);
+    resolve(h, "flare_decay_backward", lib.decay_backward);
+    resolve(h, "flare_decay_step", lib.decay_step);
+    resolve(h, "flare_residual_norm_workspace_bytes", lib.norm_workspace_bytes);
+    resolve(h, "flare_residual_norm_forward", lib.norm_forward);
+    resolve(h, "flare_residual_norm_backward", lib.norm_backward);
 }
 
 void check(int code, const char *what)
@@ -456,6 +473,513 @@ OptTensor mixer(const Tensor &q_in, const Tensor &k_in, const Tensor &v_in, doub
     return y;
 }
 
+// ---- decay mixer and residual norm --------------------------------------------------------------------------
+// What every entry point below begins with: the tensors are on one device, which is made the current one (its current
+// stream, its allocator) until the call returns.
+c10::Device one_device(const Tensor &first, const char *name, std::initializer_list<const OptTensor *> others)
+{
+    if (!first.is_cuda()) throw Error(std::string(name) + " must be a contiguous device tensor");
+    for (const OptTensor *t : others)
+        if (*t && (*t)->device() != first.device()) throw Error("tensors are not all on " + first.device().str());
+    return first.device();
+}
+OptTensor defined(const Tensor &t) { return t.defined() ? OptTensor(t) : std::nullopt; }
+// a part of a Tensor list that may be missing
+OptTensor contiguous(const OptTensor &t) { return t ? OptTensor(t->contiguous()) : std::nullopt; }
+
+// A backward pass that is captured into a graph must not meet a leaf whose gradient accumulator an eager graph still holds
+// on another stream: the engine would make the two streams wait for each other, which ends the capture and the process.
+void check_capture(std::initializer_list<const OptTensor *> inputs)
+{
+    if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
+    for (const OptTensor *t : inputs) {
+        if (!*t || !(*t)->requires_grad() || !(*t)->is_leaf()) continue;
+        const auto held = torch::autograd::impl::try_get_grad_accumulator(**t);
+        if (held && held->stream() && *held->stream() != c10::hip::getCurrentHIPStream().unwrap())
+            throw Error("a graph is being captured while an eager graph of the same leaf tensors lives: drop its outputs first");
+    }
+}
+void check_tangents(const char *what, std::initializer_list<const OptTensor *> inputs)
+{
+    for (const OptTensor *t : inputs)   // a tangent would be lost without a word
+        if (*t && (*t)->_fw_grad(0).defined()) throw Error(std::string(what) + " has no forward-mode derivative");
+}
+bool any_requires_grad(std::initializer_list<const OptTensor *> inputs)
+{
+    if (!at::GradMode::is_enabled()) return false;
+    for (const OptTensor *t : inputs)
+        if (*t && (*t)->requires_grad()) return true;
+    return false;
+}
+Tensor or_none(const OptTensor &t) { return t ? *t : Tensor(); }
+// An Error of a backward pass surfaces as the package's exception class (the engine would make it a plain RuntimeError).
+template <typename F>
+torch::autograd::variable_list raising(const F &f)
+{
+    try {
+        return f();
+    } catch (const Error &e) {
+        const py::gil_scoped_acquire gil;
+        PyErr_SetString(error_class->ptr(), e.what());
+        python_error raised;
+        raised.persist();
+        throw raised;
+    }
+}
+
+struct DecayDims {
+    std::array<int64_t, 4> state;
+    std::array<int64_t, 1> heads, items;
+    explicit DecayDims(const flare_decay_shape &s) : state{s.B, s.H, s.d, s.d}, heads{s.H}, items{s.B} {}
+};
+int dim_of(int64_t x)
+{
+    if (x > INT_MAX) throw Error("a dimension is beyond 2^31 - 1");
+    return (int)x;
+}
+flare_decay_shape decay_shape_of(const Tensor &q, int layout)
+{
+    if (q.dim() != 4) throw Error("expected q[B,H,N,d] (layout 'bhnd') or q[B,N,H,d] (layout 'bnhd')");
+    const bool heads_first = layout == FLARE_BHND;
+    flare_decay_shape s{};
+    s.B = dim_of(q.size(0));
+    s.H = dim_of(q.size(heads_first ? 1 : 2));
+    s.N = dim_of(q.size(heads_first ? 2 : 1));
+    s.d = dim_of(q.size(3));
+    s.dtype = dtype_code(q);
+    s.layout = (flare_layout)layout;
+    return s;
+}
+const float *cf32(const void *p) { return static_cast<const float *>(p); }
+const int *ci32(const void *p) { return static_cast<const int *>(p); }
+size_t decay_bytes(const flare_decay_shape &s, bool backward)
+{
+    size_t n = 0;
+    check(backward ? lib.decay_workspace_bytes(&s, nullptr, &n) : lib.decay_workspace_bytes(&s, &n, nullptr),
+          "flare_decay_workspace_bytes");
+    return n;
+}
+// Needs none: no block is asked of the allocator.
+Workspace decay_workspace(size_t need, const OptTensor &given, const Tensor &like, const Target &to)
+{
+    if (!given && need == 0) return Workspace{Tensor(), nullptr, 0};
+    return workspace_for(need, given, like, to);
+}
+
+std::tuple<Tensor, OptTensor> decay_forward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay, double scale,
+                                            const OptTensor &lengths, const OptTensor &state, const OptTensor &o_in,
+                                            const OptTensor &state_out_in, bool want_state, const OptTensor &ws_in,
+                                            const py::object &stream, int layout)
+{
+    const OptTensor ok = k, ov = v, og = log_decay;
+    const c10::DeviceGuard guard(one_device(q, "q", {&ok, &ov, &og, &lengths, &state, &o_in, &state_out_in, &ws_in}));
+    const flare_decay_shape s = decay_shape_of(q, layout);
+    const DecayDims dim(s);
+    const Target to = target(stream, !ws_in);
+    const py::gil_scoped_release no_gil;
+    const at::ScalarType dt = q.scalar_type();
+    const size_t need = decay_bytes(s, false);
+    Tensor o = out_or_new(o_in, q.sizes(), dt, q);
+    OptTensor so = state_out_in;
+    if (!so && want_state) so = new_empty(dim.state, at::kFloat, q);
+    const Workspace ws = decay_workspace(need, ws_in, q, to);
+    check(lib.decay_forward(&s, dev(q, "q"), dev(k, "k", dt, q.sizes()), dev(v, "v", dt, q.sizes()),
+                            cf32(dev(log_decay, "log_decay", at::kFloat, dim.heads)),
+                            ci32(dev(lengths, "lengths", at::kInt, dim.items)), cf32(dev(state, "state", at::kFloat, dim.state)),
+                            dev(o, "o", dt, q.sizes()), f32(dev(so, "state_out", at::kFloat, dim.state)), (float)scale, ws.ptr,
+                            ws.bytes, to.stream),
+          "flare_decay_forward");
+    return {o, so};
+}
+
+std::tuple<Tensor, Tensor, Tensor, OptTensor> decay_backward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay,
+                                                             const Tensor &d_o, double scale, const OptTensor &lengths,
+                                                             const OptTensor &state, const OptTensor &dstate_out,
+                                                             const OptTensor &dq_in, const OptTensor &dk_in, const OptTensor &dv_in,
+                                                             const OptTensor &dstate_in, bool want_dstate, const OptTensor &ws_in,
+                                                             const py::object &stream, int layout)
+{
+    const OptTensor ok = k, ov = v, og = log_decay, od = d_o;
+    const c10::DeviceGuard guard(one_device(
+        q, "q", {&ok, &ov, &og, &od, &lengths, &state, &dstate_out, &dq_in, &dk_in, &dv_in, &dstate_in, &ws_in}));
+    const flare_decay_shape s = decay_shape_of(q, layout);
+    const DecayDims dim(s);
+    const Target to = target(stream, !ws_in);
+    const py::gil_scoped_release no_gil;
+    const at::ScalarType dt = q.scalar_type();
+    const size_t need = decay_bytes(s, true);
+    Tensor dq = out_or_new(dq_in, q.sizes(), dt, q), dk = out_or_new(dk_in, q.sizes(), dt, q), dv = out_or_new(dv_in, q.sizes(), dt, q);
+    OptTensor ds = dstate_in;
+    if (!ds && want_dstate) ds = new_empty(dim.state, at::kFloat, q);
+    const Workspace ws = decay_workspace(need, ws_in, q, to);
+    check(lib.decay_backward(&s, dev(q, "q"), dev(k, "k", dt, q.sizes()), dev(v, "v", dt, q.sizes()),
+                             cf32(dev(log_decay, "log_decay", at::kFloat, dim.heads)),
+                             ci32(dev(lengths, "lengths", at::kInt, dim.items)), cf32(dev(state, "state", at::kFloat, dim.state)),
+                             dev(d_o, "d_o", dt, q.sizes()), cf32(dev(dstate_out, "dstate_out", at::kFloat, dim.state)),
+                             dev(dq, "dq", dt, q.sizes()), dev(dk, "dk", dt, q.sizes()), dev(dv, "dv", dt, q.sizes()),
+                             f32(dev(ds, "dstate_in", at::kFloat, dim.state)), (float)scale, ws.ptr, ws.bytes, to.stream),
+          "flare_decay_backward");
+    return {dq, dk, dv, ds};
+}
+
+Tensor decay_step(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay, const Tensor &state, double scale,
+                  const OptTensor &state_out, const OptTensor &active, const OptTensor &o_in, const py::object &stream)
+{
+    const OptTensor ok = k, ov = v, og = log_decay, os = state;
+    const c10::DeviceGuard guard(one_device(q, "q", {&ok, &ov, &og, &os, &state_out, &active, &o_in}));
+    if (q.dim() != 3) throw Error("expected q[B,H,d]");
+    flare_decay_shape s{};
+    s.B = dim_of(q.size(0));
+    s.H = dim_of(q.size(1));
+    s.N = 1;
+    s.d = dim_of(q.size(2));
+    s.dtype = dtype_code(q);
+    const DecayDims dim(s);
+    const Target to = target(stream, false);
+    const py::gil_scoped_release no_gil;
+    const at::ScalarType dt = q.scalar_type();
+    const Tensor &so = state_out ? *state_out : state;
+    Tensor o = out_or_new(o_in, q.sizes(), dt, q);
+    check(lib.decay_step(&s, dev(q, "q"), dev(k, "k", dt, q.sizes()), dev(v, "v", dt, q.sizes()),
+                         cf32(dev(log_decay, "log_decay", at::kFloat, dim.heads)), ci32(dev(active, "active", at::kInt, dim.items)),
+                         cf32(dev(state, "state", at::kFloat, dim.state)), f32(dev(so, "state_out", at::kFloat, dim.state)),
+                         dev(o, "o", dt, q.sizes()), (float)scale, to.stream),
+          "flare_decay_step");
+    return o;
+}
+
+struct DecayBackward : torch::autograd::Node {
+    torch::autograd::SavedVariable q, k, v, log_decay, lengths, state;
+    flare_decay_shape shape{};
+    float scale = 0.f;
+
+    std::string name() const override { return "FlareDecayBackward"; }
+    void release_variables() override
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        for (auto *t : {&q, &k, &v, &log_decay, &lengths, &state}) t->reset_data();
+    }
+    torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        return raising([&] { return gradients(std::move(grads[0]), grads.size() > 1 ? std::move(grads[1]) : Tensor()); });
+    }
+    torch::autograd::variable_list gradients(Tensor &&d_o, Tensor &&dstate)
+    {
+        const Tensor tq = q.unpack(), tk = k.unpack(), tv = v.unpack(), tg = log_decay.unpack();
+        const OptTensor tl = defined(lengths.unpack()), ts = defined(state.unpack());
+        // held against the forward's shape, as a saved-tensor hook may have handed back anything
+        const at::ScalarType dt = scalar_type(shape.dtype);
+        const bool heads_first = shape.layout == FLARE_BHND;
+        const std::array<int64_t, 4> tok{shape.B, heads_first ? shape.H : shape.N, heads_first ? shape.N : shape.H, shape.d};
+        const DecayDims dim(shape);
+        const void *const pq = dev(tq, "q", dt, tok), *const pk = dev(tk, "k", dt, tok), *const pv = dev(tv, "v", dt, tok),
+                   *const pg = dev(tg, "log_decay", at::kFloat, dim.heads), *const pl = dev(tl, "lengths", at::kInt, dim.items),
+                   *const ps = dev(ts, "state", at::kFloat, dim.state);
+        const OptTensor ok = tk, ov = tv, og = tg;
+        const c10::DeviceGuard guard(one_device(tq, "q", {&ok, &ov, &og, &tl, &ts}));
+        if (!d_o.defined()) d_o = at::zeros(tok, tq.options().requires_grad(false));   // only the state was used
+        d_o = d_o.contiguous();
+        OptTensor ds = contiguous(defined(dstate));
+        const Target to{c10::hip::getCurrentHIPStream().stream(), std::nullopt};
+        Tensor dq = new_empty(tok, dt, tq), dk = new_empty(tok, dt, tq), dv = new_empty(tok, dt, tq), dfirst;
+        if (ts && task_should_compute_output(3)) dfirst = new_empty(dim.state, at::kFloat, tq);
+        const Workspace ws = decay_workspace(decay_bytes(shape, true), std::nullopt, tq, to);
+        check(lib.decay_backward(&shape, pq, pk, pv, cf32(pg), ci32(pl), cf32(ps), dev(d_o, "the gradient of o", dt, tok),
+                                 cf32(dev(ds, "the gradient of the state", at::kFloat, dim.state)), dq.data_ptr(), dk.data_ptr(),
+                                 dv.data_ptr(), dfirst.defined() ? f32(dfirst.data_ptr()) : nullptr, scale, ws.ptr, ws.bytes,
+                                 to.stream),
+              "flare_decay_backward");
+        return {dq, dk, dv, dfirst};
+    }
+};
+
+// Nothing under torch.jit.trace, as for the mixer.
+std::optional<std::tuple<Tensor, OptTensor>> decay_mixer(const Tensor &q_in, const Tensor &k_in, const Tensor &v_in,
+                                                         const Tensor &log_decay_in, double scale, const OptTensor &lengths_in,
+                                                         const OptTensor &state_in, bool want_state, int layout)
+{
+    if (torch::jit::tracer::isTracing()) return std::nullopt;
+    const OptTensor oq = q_in, ok = k_in, ov = v_in, og = log_decay_in;
+    const c10::DeviceGuard guard(one_device(q_in, "q", {&ok, &ov, &og, &lengths_in, &state_in}));
+    check_tangents("decay_mixer", {&oq, &ok, &ov, &og, &state_in});
+    if (at::GradMode::is_enabled() && log_decay_in.requires_grad())
+        throw Error("log_decay is not differentiated: pass it detached");
+    std::shared_ptr<DecayBackward> node;
+    if (any_requires_grad({&oq, &ok, &ov, &state_in})) {
+        check_capture({&oq, &ok, &ov, &state_in});
+        node = std::shared_ptr<DecayBackward>(new DecayBackward(), torch::autograd::deleteNode);
+        node->set_next_edges(torch::autograd::collect_next_edges(q_in, k_in, v_in, or_none(state_in)));
+    }
+    Tensor q = q_in, k = k_in, v = v_in, log_decay = log_decay_in;
+    OptTensor lengths = lengths_in, state = state_in;
+    {
+        const at::AutoDispatchBelowADInplaceOrView below;   // not around the saving: saved-tensor hooks run there
+        q = q.contiguous();
+        k = k.contiguous();
+        v = v.contiguous();
+        log_decay = log_decay.contiguous();
+        lengths = contiguous(lengths);
+        state = contiguous(state);
+    }
+    const flare_decay_shape s = decay_shape_of(q, layout);
+    const DecayDims dim(s);
+    const at::ScalarType dt = q.scalar_type();
+    const Target to{c10::hip::getCurrentHIPStream().stream(), std::nullopt};
+    const size_t need = decay_bytes(s, false);
+    Tensor o = new_empty(q.sizes(), dt, q), state_out;
+    if (want_state) state_out = new_empty(dim.state, at::kFloat, q);
+    const Workspace ws = decay_workspace(need, std::nullopt, q, to);
+    check(lib.decay_forward(&s, dev(q, "q"), dev(k, "k", dt, q.sizes()), dev(v, "v", dt, q.sizes()),
+                            cf32(dev(log_decay, "log_decay", at::kFloat, dim.heads)),
+                            ci32(dev(lengths, "lengths", at::kInt, dim.items)), cf32(dev(state, "state", at::kFloat, dim.state)),
+                            o.data_ptr(), want_state ? f32(state_out.data_ptr()) : nullptr, (float)scale, ws.ptr, ws.bytes, to.stream),
+          "flare_decay_forward");
+    if (node) {
+        node->shape = s;
+        node->scale = (float)scale;
+        node->q = torch::autograd::SavedVariable(q, false);
+        node->k = torch::autograd::SavedVariable(k, false);
+        node->v = torch::autograd::SavedVariable(v, false);
+        node->log_decay = torch::autograd::SavedVariable(log_decay, false);
+        node->lengths = torch::autograd::SavedVariable(or_none(lengths), false);
+        node->state = torch::autograd::SavedVariable(or_none(state), false);
+        torch::autograd::set_history(o, node);
+        if (want_state) torch::autograd::set_history(state_out, node);
+    }
+    return std::make_tuple(o, defined(state_out));
+}
+
+// What a residual norm is made of, besides x, y and the gate.
+struct NormParts {
+    OptTensor pre_w, pre_b, post_w, post_b;
+};
+struct NormCall {
+    flare_norm_shape s{};
+    std::vector<int64_t> gate_dim;
+};
+// `dt`: the type of h where there is no y
+NormCall norm_call(const Tensor &x, const OptTensor &y, const OptTensor &gate, int pre, int post, int act, const std::optional<at::ScalarType> &dt)
+{
+    if (x.dim() < 1) throw Error("x must have a dimension of channels");
+    NormCall c;
+    flare_norm_shape &s = c.s;
+    const at::ScalarType type = y ? y->scalar_type() : dt ? *dt : x.scalar_type();
+    s.C = dim_of(x.size(-1));
+    if (s.C < 1 || x.numel() < 1) throw Error("x is empty");
+    s.rows = x.numel() / s.C;
+    s.dtype = type == at::kFloat ? FLARE_F32 : type == at::kBFloat16 ? FLARE_BF16 : type == at::kHalf ? FLARE_F16 : dtype_code(y ? *y : x);
+    s.x_f32 = x.scalar_type() == at::kFloat && s.dtype != FLARE_F32;
+    if (!s.x_f32 && x.scalar_type() != type) throw Error("x must have the type of y, or float32");
+    s.pre = (flare_norm)pre;
+    s.post = (flare_norm)post;
+    s.gate = gate ? (flare_gate)act : FLARE_GATE_NONE;
+    s.rows_per_gate = 1;
+    if (gate) {
+        // x's shape, [C], or x's shape with ones where the rows share it (ones behind everything they do not share)
+        const auto g = gate->sizes(), t = x.sizes();
+        c.gate_dim.assign(g.begin(), g.end());
+        if (g.size() == 1 && t.size() > 1) {
+            if (g[0] != s.C) throw Error("gate must have shape (" + std::to_string(s.C) + ",)");
+            s.rows_per_gate = s.rows;
+        } else {
+            bool fits = g.size() == t.size() && g.back() == s.C;
+            long long shared = 1;
+            size_t i = fits ? g.size() - 1 : 0;
+            for (; fits && i > 0 && g[i - 1] == 1; --i) shared *= t[i - 1];
+            for (; fits && i > 0; --i) fits = g[i - 1] == t[i - 1];
+            if (!fits)
+                throw Error("gate must have x's shape " + text(t) + ", that shape with ones in the last of the dimensions before the "
+                            "channels, or (" + std::to_string(s.C) + ",), got " + text(g));
+            s.rows_per_gate = shared;
+        }
+    }
+    return c;
+}
+struct NormParams {
+    flare_norm_params p{};
+    NormParams(const NormParts &t, int64_t C)
+    {
+        const std::array<int64_t, 1> dim{C};
+        p.pre_weight = cf32(dev(t.pre_w, "pre_weight", at::kFloat, dim));
+        p.pre_bias = cf32(dev(t.pre_b, "pre_bias", at::kFloat, dim));
+        p.post_weight = cf32(dev(t.post_w, "post_weight", at::kFloat, dim));
+        p.post_bias = cf32(dev(t.post_b, "post_bias", at::kFloat, dim));
+    }
+};
+void *dev_or_null(const OptTensor &t, const char *name) { return t ? dev(*t, name) : nullptr; }
+std::array<int64_t, 2> stats_dim(const flare_norm_shape &s) { return {s.rows, 4}; }
+
+std::tuple<OptTensor, OptTensor> norm_forward(const Tensor &x, const OptTensor &y, const OptTensor &gate, int pre, int post, int act,
+                                              const OptTensor &pre_w, const OptTensor &pre_b, const OptTensor &post_w,
+                                              const OptTensor &post_b, double alpha, double eps, const OptTensor &x_out_in,
+                                              const OptTensor &h_in, const OptTensor &stats, const std::optional<at::ScalarType> &h_dtype,
+                                              const py::object &stream)
+{
+    const c10::DeviceGuard guard(
+        one_device(x, "x", {&y, &gate, &pre_w, &pre_b, &post_w, &post_b, &x_out_in, &h_in, &stats}));
+    const NormCall c = norm_call(x, y, gate, pre, post, act, h_in && !y ? std::optional(h_in->scalar_type()) : h_dtype);
+    const flare_norm_shape &s = c.s;
+    const Target to = target(stream, false);
+    const py::gil_scoped_release no_gil;
+    const at::ScalarType dt = scalar_type(s.dtype);
+    OptTensor x_out = x_out_in, h = h_in;
+    if (!x_out && y) x_out = new_empty(x.sizes(), x.scalar_type(), x);
+    if (!h && pre != FLARE_NORM_NONE) h = new_empty(x.sizes(), dt, x);
+    const NormParams p(NormParts{pre_w, pre_b, post_w, post_b}, s.C);
+    check(lib.norm_forward(&s, &p.p, dev(x, "x"), dev(y, "y", dt, x.sizes()), dev(gate, "gate", dt, c.gate_dim),
+                           dev(x_out, "x_out", x.scalar_type(), x.sizes()), dev(h, "h", dt, x.sizes()),
+                           f32(dev(stats, "stats", at::kFloat, stats_dim(s))), (float)alpha, (float)eps, to.stream),
+          "flare_residual_norm_forward");
+    return {x_out, h};
+}
+
+using NormGrads = std::array<OptTensor, 7>;   // of x, y, gate, pre_weight, pre_bias, post_weight, post_bias
+size_t norm_bytes(const flare_norm_shape &s)
+{
+    size_t n = 0;
+    check(lib.norm_workspace_bytes(&s, &n), "flare_residual_norm_workspace_bytes");
+    return n;
+}
+NormGrads norm_gradients(const NormCall &c, const Tensor &x, const OptTensor &y, const OptTensor &gate, const NormParts &parts,
+                         const OptTensor &stats, const OptTensor &dx_out, const OptTensor &dh, double alpha,
+                         const std::array<bool, 7> &want, const OptTensor &ws_in, const Target &to)
+{
+    const flare_norm_shape &s = c.s;
+    const at::ScalarType dt = scalar_type(s.dtype);
+    const std::array<int64_t, 1> channels{s.C};
+    const NormParams p(parts, s.C);
+    NormGrads g;
+    if (want[0]) g[0] = new_empty(x.sizes(), x.scalar_type(), x);
+    if (want[1] && y) g[1] = new_empty(x.sizes(), dt, x);
+    if (want[2] && gate) g[2] = new_empty(c.gate_dim, dt, x);
+    const OptTensor *const params[4] = {&parts.pre_w, &parts.pre_b, &parts.post_w, &parts.post_b};
+    for (int i = 0; i < 4; ++i)
+        if (want[3 + i] && *params[i]) g[3 + i] = new_empty(channels, at::kFloat, x);
+    const auto ptr = [&](int i) { return g[i] ? g[i]->data_ptr() : nullptr; };
+    const Workspace ws = workspace_for(norm_bytes(s), ws_in, x, to);
+    check(lib.norm_backward(&s, &p.p, dev(x, "x"), dev(y, "y", dt, x.sizes()), dev(gate, "gate", dt, c.gate_dim),
+                            cf32(dev(stats, "stats", at::kFloat, stats_dim(s))), dev(dx_out, "dx_out", x.scalar_type(), x.sizes()),
+                            dev(dh, "dh", dt, x.sizes()), ptr(0), ptr(1), ptr(2), f32(ptr(3)), f32(ptr(4)), f32(ptr(5)), f32(ptr(6)),
+                            (float)alpha, ws.ptr, ws.bytes, to.stream),
+          "flare_residual_norm_backward");
+    return g;
+}
+
+NormGrads norm_backward(const Tensor &x, const OptTensor &y, const OptTensor &dx_out, const OptTensor &dh, const OptTensor &stats,
+                        const OptTensor &gate, int pre, int post, int act, const OptTensor &pre_w, const OptTensor &pre_b,
+                        const OptTensor &post_w, const OptTensor &post_b, double alpha, const OptTensor &ws_in,
+                        const py::object &stream)
+{
+    const c10::DeviceGuard guard(
+        one_device(x, "x", {&y, &dx_out, &dh, &stats, &gate, &pre_w, &pre_b, &post_w, &post_b, &ws_in}));
+    const NormCall c = norm_call(x, y, gate, pre, post, act, dh ? std::optional(dh->scalar_type()) : std::nullopt);
+    const Target to = target(stream, !ws_in);
+    const py::gil_scoped_release no_gil;
+    return norm_gradients(c, x, y, gate, NormParts{pre_w, pre_b, post_w, post_b}, stats, dx_out, dh, alpha,
+                          {true, true, true, true, true, true, true}, ws_in, to);
+}
+
+struct NormBackward : torch::autograd::Node {
+    torch::autograd::SavedVariable x, y, gate, pre_w, pre_b, post_w, post_b, stats;
+    NormCall call;
+    std::vector<int64_t> x_dim;
+    bool has_y = false, has_h = false, has_stats = false;
+    double alpha = 1.0;
+
+    std::string name() const override { return "FlareResidualNormBackward"; }
+    void release_variables() override
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        for (auto *t : {&x, &y, &gate, &pre_w, &pre_b, &post_w, &post_b, &stats}) t->reset_data();
+    }
+    torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        return raising([&] { return gradients(std::move(grads)); });
+    }
+    torch::autograd::variable_list gradients(torch::autograd::variable_list &&grads)
+    {
+        // (the outputs are x_out, if there is a y, and h, if there is a pre norm)
+        OptTensor dx_out = has_y ? contiguous(defined(grads[0])) : std::nullopt,
+                  dh = has_h ? contiguous(defined(grads[has_y ? 1 : 0])) : std::nullopt;
+        const Tensor tx = x.unpack();
+        const OptTensor ty = defined(y.unpack()), tg = defined(gate.unpack()), ts = defined(stats.unpack());
+        const NormParts parts{defined(pre_w.unpack()), defined(pre_b.unpack()), defined(post_w.unpack()), defined(post_b.unpack())};
+        const c10::DeviceGuard guard(
+            one_device(tx, "x", {&ty, &tg, &ts, &parts.pre_w, &parts.pre_b, &parts.post_w, &parts.post_b}));
+        dev(tx, "x", call.s.x_f32 ? at::kFloat : scalar_type(call.s.dtype), x_dim);   // (the rest is held against x below)
+        if (ty.has_value() != has_y || tg.has_value() != (call.s.gate != FLARE_GATE_NONE) || ts.has_value() != has_stats)
+            throw Error("a saved tensor is missing");
+        std::array<bool, 7> want;
+        for (int i = 0; i < 7; ++i) want[i] = task_should_compute_output(i);
+        const Target to{c10::hip::getCurrentHIPStream().stream(), std::nullopt};
+        const NormGrads g = norm_gradients(call, tx, ty, tg, parts, ts, dx_out, dh, alpha, want, std::nullopt, to);
+        torch::autograd::variable_list out;
+        for (const OptTensor &t : g) out.push_back(or_none(t));
+        return out;
+    }
+};
+
+std::optional<std::tuple<OptTensor, OptTensor>> residual_norm(const Tensor &x_in, const OptTensor &y_in, const OptTensor &gate_in, int pre,
+                                                             int post, int act, const OptTensor &pre_w_in, const OptTensor &pre_b_in,
+                                                             const OptTensor &post_w_in, const OptTensor &post_b_in, double alpha,
+                                                             double eps, const std::optional<at::ScalarType> &h_dtype)
+{
+    if (torch::jit::tracer::isTracing()) return std::nullopt;
+    const OptTensor ox = x_in;
+    const c10::DeviceGuard guard(
+        one_device(x_in, "x", {&y_in, &gate_in, &pre_w_in, &pre_b_in, &post_w_in, &post_b_in}));
+    check_tangents("residual_norm", {&ox, &y_in, &gate_in, &pre_w_in, &pre_b_in, &post_w_in, &post_b_in});
+    std::shared_ptr<NormBackward> node;
+    if (any_requires_grad({&ox, &y_in, &gate_in, &pre_w_in, &pre_b_in, &post_w_in, &post_b_in})) {
+        check_capture({&ox, &y_in, &gate_in, &pre_w_in, &pre_b_in, &post_w_in, &post_b_in});
+        node = std::shared_ptr<NormBackward>(new NormBackward(), torch::autograd::deleteNode);
+        node->set_next_edges(torch::autograd::collect_next_edges(x_in, or_none(y_in), or_none(gate_in), or_none(pre_w_in),
+                                                                 or_none(pre_b_in), or_none(post_w_in), or_none(post_b_in)));
+    }
+    Tensor x = x_in;
+    OptTensor y = y_in, gate = gate_in;
+    NormParts parts{pre_w_in, pre_b_in, post_w_in, post_b_in};
+    {
+        const at::AutoDispatchBelowADInplaceOrView below;
+        x = x.contiguous();
+        for (OptTensor *t : {&y, &gate, &parts.pre_w, &parts.pre_b, &parts.post_w, &parts.post_b}) *t = contiguous(*t);
+    }
+    const NormCall c = norm_call(x, y, gate, pre, post, act, h_dtype);
+    const flare_norm_shape &s = c.s;
+    const at::ScalarType dt = scalar_type(s.dtype);
+    const Target to{c10::hip::getCurrentHIPStream().stream(), std::nullopt};
+    OptTensor x_out, h, stats;
+    if (y) x_out = new_empty(x.sizes(), x.scalar_type(), x);
+    if (pre != FLARE_NORM_NONE) h = new_empty(x.sizes(), dt, x);
+    if (node && (pre != FLARE_NORM_NONE || post != FLARE_NORM_NONE)) stats = new_empty(stats_dim(s), at::kFloat, x);
+    const NormParams p(parts, s.C);
+    check(lib.norm_forward(&s, &p.p, dev(x, "x"), dev(y, "y", dt, x.sizes()), dev(gate, "gate", dt, c.gate_dim),
+                           dev_or_null(x_out, "x_out"), dev_or_null(h, "h"), f32(dev_or_null(stats, "stats")), (float)alpha, (float)eps,
+                           to.stream),
+          "flare_residual_norm_forward");
+    if (node) {
+        node->call = c;
+        node->x_dim.assign(x.sizes().begin(), x.sizes().end());
+        node->has_y = y.has_value();
+        node->has_h = h.has_value();
+        node->has_stats = stats.has_value();
+        node->alpha = alpha;
+        node->x = torch::autograd::SavedVariable(x, false);
+        node->y = torch::autograd::SavedVariable(or_none(y), false);
+        node->gate = torch::autograd::SavedVariable(or_none(gate), false);
+        node->pre_w = torch::autograd::SavedVariable(or_none(parts.pre_w), false);
+        node->pre_b = torch::autograd::SavedVariable(or_none(parts.pre_b), false);
+        node->post_w = torch::autograd::SavedVariable(or_none(parts.post_w), false);
+        node->post_b = torch::autograd::SavedVariable(or_none(parts.post_b), false);
+        node->stats = torch::autograd::SavedVariable(or_none(stats), false);
+        if (x_out) torch::autograd::set_history(*x_out, node);
+        if (h) torch::autograd::set_history(*h, node);
+    }
+    return std::make_tuple(x_out, h);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_native, m)
@@ -480,4 +1004,11 @@ PYBIND11_MODULE(_native, m)
     m.def("forward_project", &forward_project);
     m.def("backward", &backward);
     m.def("mixer", &mixer, py::call_guard<py::gil_scoped_release>());
+    m.def("decay_forward", &decay_forward);
+    m.def("decay_backward", &decay_backward);
+    m.def("decay_step", &decay_step);
+    m.def("decay_mixer", &decay_mixer, py::call_guard<py::gil_scoped_release>());
+    m.def("residual_norm_forward", &norm_forward);
+    m.def("residual_norm_backward", &norm_backward);
+    m.def("residual_norm", &residual_norm, py::call_guard<py::gil_scoped_release>());
 }
