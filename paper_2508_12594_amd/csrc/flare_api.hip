@@ -41,7 +41,8 @@ const char *const kKernelNames[KID_COUNT] = {
     "encode_partial", "encode_merge", "decode", "bwd_token_stats", "bwd_prep", "bwd_dz_partial",
     "bwd_dz_merge", "bwd_dq_partial", "bwd_dq_reduce", "bwd_dkdv",
     "decode_merge", "spectral_gram", "spectral_reduce", "spectral_eigen",
-    "spectral_post", "decode_project", "decay_sum", "decay_carry", "decay_forward", "decay_backward", "decay_step",
+    "spectral_post", "decode_project", "decay_sum", "decay_carry", "decay_forward", "decay_dq", "decay_dkdv",
+    "decay_step",
     "norm_forward", "norm_backward", "norm_sum"};
 }  // namespace
 

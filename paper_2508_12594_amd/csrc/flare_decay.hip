@@ -12,11 +12,15 @@
 // its matrix accumulators (fp32) from the first token of its segment to the last.  Per 32 tokens, with the layouts of
 // v_mfma_f32_32x32x16 (flare_mfma_common.h):
 //   P^T = Y X^T            lane = token of x, registers = tokens of y; weighted by l^(t-u) (0 above the diagonal)
-//   O^T = C^T X^T          the state's accumulators, rounded, are the A operand as they lie: a contraction index in
-//                          accumulator order, which X's rows are read in too
-//   O^T += Z^T P^T         likewise P^T's accumulators are the B operand
-//   C   += Y^T (weight Z)  Y and Z read down their columns (transposing LDS reads)
-// so that nothing but the three token tiles passes through LDS.
+//   O^T = C^T X^T          the state's accumulators, rounded, are the A operand as they lie
+//   O^T += Z^T P^T         likewise P^T's accumulators are the B operand: a contraction index in accumulator order
+//   C   += Y^T (weight Z)  Y and Z read down their columns (transposing LDS reads), Y's columns in the order that makes the
+//                          state's registers eight neighbouring rows (state_row)
+// so that nothing but the token tiles passes through LDS.  These come by direct loads into LDS, two or three chunks ahead.
+// dK and dV share their four tiles: a workgroup of theirs has waves in two roles.
+//
+// Where (b,h) are too few to fill the chip the tokens are cut into segments: a first pass takes each segment's own sum, a
+// second turns the sums into the states before the segments, a third is the scan.
 #include "flare_mfma_common.h"
 
 namespace flare {
@@ -61,17 +65,18 @@ __device__ __forceinline__ float elem_of(const Frag<DT> &f, int e)
     else return (e & 1) ? elem_hi<DT == FLARE_F16>(f.w[e >> 1]) : elem_lo<DT == FLARE_F16>(f.w[e >> 1]);
 }
 
-struct ScanJob {
-    const void *x, *y, *z;
+// What a wave does: which of the loaded tiles it takes for x, y and z, and where its states and results go.
+struct Role {
     void *out;
     const float *first;    // state before the first token, [B][H][d][d], or NULL (zero)
     float *last;           // state behind the last token, or NULL
-    float p, w, m;         // see above
-    int reverse;           // tokens from the last to the first (then lead = 0)
-    int first_turned;      // `first` is the transposed state
+    int turned;            // `first` and the slots hold the transposed state
 };
 struct ScanArgs {
-    ScanJob job[3];
+    const void *in[2][4];     // the tiles of either job (two jobs only where segments are summed)
+    Role role[2];
+    float p, w, m[2];         // see above; m of either job
+    int reverse[2];           // tokens from the last to the first (then lead = 0)
     const float *log_decay;   // [H]
     const int *lengths;       // [B] or NULL
     float *slots;             // [job][B*H][segments][d][d]: a segment's own sum, then the state before it
@@ -79,54 +84,112 @@ struct ScanArgs {
     int H, N, BH, segments, seg_len;
 };
 
-template <int DT, int D>
-struct Tile {
-    static constexpr int DP = D < 32 ? 32 : D;              // columns in LDS (d = 16: the upper 16 stay zero)
-    static constexpr int WAVES = DP / 32, THREADS = 64 * WAVES;
+// SUM: a segment's own sum (tiles y, z); FORWARD: one role (x, y, z), also dQ; DKDV: two (q, k, v, dO).
+enum ScanKind { SUM = 0, FORWARD = 1, DKDV = 2 };
+
+template <int DT, int D, int KIND>
+struct Scan {
+    static constexpr int CT = D < 32 ? 1 : D / 32;                 // blocks of 32 columns (and of 32 rows of the state)
+    static constexpr int ROLES = KIND == DKDV ? 2 : 1, TILES = KIND == SUM ? 2 : KIND == FORWARD ? 3 : 4;
+    static constexpr int WAVES = CT * ROLES, THREADS = 64 * WAVES;
     static constexpr int ES = DT == FLARE_F32 ? 4 : 2;
-    static constexpr int ROW = DP * ES + 16, BYTES = 32 * ROW;
-    static constexpr int ROW_PIECES = D * ES / 16, PIECES = 32 * ROW_PIECES / THREADS;   // 16-byte pieces, and each thread's
-    static constexpr int BUFFERS = 6 * BYTES <= 64 * 1024 ? 2 : 1;
-    // planes of the weighted z: what the state sums is good to 2^-22 (fp16) or 2^-24 (bf16) of a term
-    static constexpr int PLANES = DT == FLARE_F32 ? 1 : DT == FLARE_F16 ? 2 : 3;
+    static constexpr int ROW = D * ES, BYTES = 32 * ROW, SET = TILES * BYTES;
+    static constexpr int PIECES = ROW / 16;                        // of a row
+    static constexpr int TILE_LOADS = BYTES / 1024;                // wave-wide loads of a tile; those of all tiles go round the waves
+    static constexpr int LOADS = TILES * TILE_LOADS / WAVES;       // and so many of them are each wave's
+    // Chunks held in LDS: as many as leave room for eight waves on a CU, two at least, four at most.
+    static constexpr int FIT = 160 * 1024 / (SET * (WAVES < 8 ? 8 / WAVES : 1));
+    static constexpr int STAGES = FIT < 2 ? 2 : FIT > 4 ? 4 : FIT;
+    static constexpr int STORES = KIND == SUM ? 0 : (D < 32 ? 1 : 2) * (ES / 2);   // of a wave, each full chunk
+    static constexpr int PER_SIMD = WAVES * (160 * 1024 / (STAGES * SET)) >= 8 ? 2 : 1;   // waves (fp32, d = 128: one)
+    static_assert(TILES * TILE_LOADS % WAVES == 0 && STAGES * SET <= 160 * 1024, "");
 };
 
 // One head's decay in log2 units per token.  (Far below what fp32 weights resolve it makes no difference, and 0 * inf would.)
 __device__ __forceinline__ float decay_log2(float g) { return g <= 0.f ? fmaxf(g * kLog2e, -3000.f) : __builtin_nanf(""); }
 __device__ __forceinline__ int item_length(const int *lengths, int b, int N) { return lengths ? min(max(lengths[b], 0), N) : N; }
 
+// l^n for a factor that is applied again and again: the two fp32 numbers around it, of which `next` gives the one that takes
+// the product of all factors so far back towards the exact power.  (One of them alone is off by up to 2^-25, always the same
+// way: 2^-18 after a hundred chunks.)
+struct Fade {
+    float up, down, err_up, err_down, drift;
+    __device__ __forceinline__ Fade(float g, int n)
+    {
+        const double exact = g <= 0.f ? exp(fmax((double)g, -2080.0) * n) : (double)__builtin_nanf("");
+        up = down = (float)exact;
+        if ((double)up < exact) up = __uint_as_float(__float_as_uint(up) + 1);
+        else if ((double)down > exact) down = __uint_as_float(__float_as_uint(down) - 1);
+        err_up = exact > 0.0 ? (float)((double)up / exact - 1.0) : 0.f;
+        err_down = exact > 0.0 ? (float)((double)down / exact - 1.0) : 0.f;
+        drift = 0.f;
+    }
+    __device__ __forceinline__ float next()
+    {
+        const bool high = drift < 0.f;
+        drift += high ? err_up : err_down;
+        return high ? up : down;
+    }
+};
+
+// Rows lie in LDS one behind the other (the direct loads write 1024 bytes in lane order), so that a column would lie in few
+// banks: the 16-byte pieces of row r change places, piece c lying at c ^ swizzle(r).  Sixteen rows of a 16-byte read, and four
+// rows of a transposing one, then lie in different banks.
+template <int ROW>
+__device__ __forceinline__ int swizzle(int r)
+{
+    if constexpr (ROW >= 256) return (r & 7) << 1 | (r >> 3 & 1);
+    else if constexpr (ROW == 128) return (r >> 1 & 3) << 1 | (r >> 3 & 1);
+    else if constexpr (ROW == 64) return r >> 2 & 3;
+    else return r >> 3 & 1;
+}
+template <int ROW>
+__device__ __forceinline__ const char *piece_at(const char *tile, int r, int c) { return tile + r * ROW + ((c ^ swizzle<ROW>(r)) << 4); }
+
+// Row `row`, columns 16 s + 8 hh + 0..7
 template <int DT, int D>
 __device__ __forceinline__ Frag<DT> row_frag(const char *tile, int row, int s, int hh)
 {
-    using T = Tile<DT, D>;
-    const char *p = tile + row * T::ROW + (16 * s + 4 * hh) * T::ES;
+    constexpr int ROW = D * (DT == FLARE_F32 ? 4 : 2);
     Frag<DT> f;
     if constexpr (DT == FLARE_F32) {
-        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 32);
+        const float4 a = *reinterpret_cast<const float4 *>(piece_at<ROW>(tile, row, 4 * s + 2 * hh)),
+                     b = *reinterpret_cast<const float4 *>(piece_at<ROW>(tile, row, 4 * s + 2 * hh + 1));
         f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
         f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
     } else {
-        const u32x2 a = *reinterpret_cast<const u32x2 *>(p), b = *reinterpret_cast<const u32x2 *>(p + 16);
-        f.w[0] = a[0]; f.w[1] = a[1]; f.w[2] = b[0]; f.w[3] = b[1];
+        f.w = *reinterpret_cast<const u32x4 *>(piece_at<ROW>(tile, row, 2 * s + hh));
     }
     return f;
 }
-// Column 32 * ct + lane % 32 of the tile, 8 tokens of step ks in accumulator order
-template <int DT, int D>
+// Row m of the A operand Y^T is this column of Y: accumulator register r of the product then holds row
+// 16 (r/8) + 8 hh + r % 8 of the state, eight neighbours for each step of 16 (what row_frag reads).
+__device__ __forceinline__ int state_col(int m) { return (m & 16) + 8 * (m >> 2 & 1) + 4 * (m >> 3 & 1) + (m & 3); }
+__device__ __forceinline__ int state_row(int ct, int r, int hh) { return 32 * ct + 16 * (r >> 3) + 8 * hh + (r & 7); }
+// 32 columns from 32 * ct, 8 tokens of step ks in accumulator order: lane % 32 = column, or (STATE) row of Y^T as above
+template <int DT, int D, bool STATE>
 __device__ __forceinline__ Frag<DT> col_frag(const char *tile, int ct, int ks, int lane)
 {
-    using T = Tile<DT, D>;
+    constexpr int ROW = D * (DT == FLARE_F32 ? 4 : 2);
     Frag<DT> f;
     if constexpr (DT == FLARE_F32) {
-        const char *p = tile + (32 * ct + (lane & 31)) * 4 + (16 * ks + 4 * (lane >> 5)) * T::ROW;
+        int c = lane & 31;
+        if constexpr (STATE) c = state_col(c);
+        if constexpr (D < 32) c &= 15;
+        const int t = 16 * ks + 4 * (lane >> 5);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f.v[e] = *reinterpret_cast<const float *>(p + (8 * (e >> 2) + (e & 3)) * T::ROW);
+        for (int e = 0; e < 8; ++e) {
+            const float x = *reinterpret_cast<const float *>(piece_at<ROW>(tile, t + 8 * (e >> 2) + (e & 3), 8 * ct + (c >> 2)) + 4 * (c & 3));
+            f.v[e] = D < 32 && (lane & 16) ? 0.f : x;
+        }
     } else {
-        const int g = lane >> 4, q = lane & 15;
-        const char *p = tile + (16 * ks + 4 * (g >> 1) + (q >> 2)) * T::ROW + (32 * ct + 16 * (g & 1) + 4 * (q & 3)) * 2;
-        const u32x2 a = lds_read_tr16(reinterpret_cast<const uint16_t *>(p));
-        const u32x2 b = lds_read_tr16(reinterpret_cast<const uint16_t *>(p + 8 * T::ROW));
+        const int g = lane >> 4, q = lane & 15, pc = q & 3, t = 16 * ks + 4 * (g >> 1) + (q >> 2);
+        const int block = D < 32 ? 0 : 4 * ct + 2 * (g & 1);
+        const int c = block + (STATE ? pc & 1 : pc >> 1), at = 8 * (STATE ? pc >> 1 : pc & 1);
+        const u32x2 a = lds_read_tr16(reinterpret_cast<const uint16_t *>(piece_at<ROW>(tile, t, c) + at));
+        const u32x2 b = lds_read_tr16(reinterpret_cast<const uint16_t *>(piece_at<ROW>(tile, t + 8, c) + at));
         f.w[0] = a[0]; f.w[1] = a[1]; f.w[2] = b[0]; f.w[3] = b[1];
+        if (D < 32 && (g & 1)) f.w = u32x4{0, 0, 0, 0};      // d = 16: the upper half of the block is not there
     }
     return f;
 }
@@ -141,117 +204,137 @@ __device__ __forceinline__ void fit_exponent(int &e, float largest)
     while (some && e > -96 && !__any(ldexpf(largest, -e) > 4.f)) e -= 12;
 }
 
-// SUM: only the segment's own sum (the state it adds), into its slot.
-template <int DT, int D, bool SUM>
-__global__ __launch_bounds__((Tile<DT, D>::THREADS), 2) void decay_scan_kernel(const ScanArgs a)
+// EXACT: the state is an output.  PLANES of the weighted z: what the state sums is then good to 2^-22 (fp16) or 2^-24 (bf16)
+// of a term; otherwise, as it only meets x rounded to 16 bits, to 2^-16 with bf16.
+template <int DT, int D, int KIND, bool EXACT>
+__global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::PER_SIMD)) void decay_scan_kernel(const ScanArgs a)
 {
-    using T = Tile<DT, D>;
-    constexpr int STEPS = D / 16, CT = T::DP / 32;
+    using T = Scan<DT, D, KIND>;
+    constexpr int STEPS = D / 16, CT = T::CT;
     constexpr bool F16 = DT == FLARE_F16;
-    __shared__ __align__(16) char lds[T::BUFFERS * 3 * T::BYTES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hh = lane >> 5;
-    const int seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, h = bh % a.H;
-    const ScanJob &job = a.job[blockIdx.y];
-    const bool reverse = job.reverse != 0;
+    constexpr int PLANES = DT == FLARE_F32 ? 1 : DT == FLARE_BF16 && EXACT ? 3 : 2;
+    __shared__ __align__(1024) char lds[T::STAGES * T::SET];
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave % CT, which = wave / CT;
+    // Neighbouring heads of a segment on one XCD (workgroups go round the eight): with [B][N][H][d] their rows share lines.
+    const int total = a.BH * a.segments, each = gridDim.x >> 3, work = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    if (work >= total) return;
+    const int seg = work / a.BH, bh = work % a.BH, h = bh % a.H, job = blockIdx.y;
+    const Role &role = a.role[which];
+    const bool reverse = a.reverse[job] != 0;
     const int lead = reverse ? 0 : 1;
     const int len = item_length(a.lengths, bh / a.H, a.N);
     const int t_begin = seg * a.seg_len, t_end = min(t_begin + a.seg_len, len);
     const size_t base = tok_base(a.ts, bh, a.H);
-    const float e2 = decay_log2(a.log_decay[h]);
+    const float g = a.log_decay[h], e2 = decay_log2(g);
 
-    if constexpr (SUM) {
+    if constexpr (KIND == SUM) {
         if (t_begin + a.seg_len >= len) return;       // nobody reads the sum of the last segment
     } else {
         // rows of the padding
         const int z0 = max(t_begin, len), z1 = min(t_begin + a.seg_len, a.N);
-        for (int q = tid; q < (z1 - z0) * T::ROW_PIECES; q += T::THREADS)
-            *reinterpret_cast<u32x4 *>(static_cast<char *>(job.out) +
-                                       (base + tok_off(a.ts, z0 + q / T::ROW_PIECES)) * T::ES + q % T::ROW_PIECES * 16) = u32x4{0, 0, 0, 0};
+        for (int q = tid % (64 * CT); q < (z1 - z0) * T::PIECES; q += 64 * CT)
+            *reinterpret_cast<u32x4 *>(static_cast<char *>(role.out) + (base + tok_off(a.ts, z0 + q / T::PIECES)) * T::ES +
+                                       q % T::PIECES * 16) = u32x4{0, 0, 0, 0};
         if (seg != 0 && t_begin >= len) return;
     }
-    const size_t slot = (((size_t)blockIdx.y * a.BH + bh) * a.segments + seg) * (D * D);
 
-    // the state before the segment: column 32 wave + l32, rows in accumulator order
+    // ---- loads of a chunk: 16 bytes a lane, 1024 a wave, straight into LDS ----
+    const unsigned row_bytes = (unsigned)a.ts.sn * T::ES;
+    const auto offset_of = [&](int i, int valid) {      // of load i, from the chunk's first row in memory
+        const int q = (i * T::WAVES + wave) % T::TILE_LOADS * 64 + lane, r = q / T::PIECES;
+        const int c = (q % T::PIECES) ^ swizzle<T::ROW>(r), rc = min(r, valid - 1);   // behind the end: the last row again
+        return (unsigned)(reverse ? 31 - rc : rc) * row_bytes + 16 * c;
+    };
+    unsigned offset[T::LOADS];
+#pragma unroll
+    for (int i = 0; i < T::LOADS; ++i) offset[i] = offset_of(i, 32);
+    const auto load = [&](int t0, int stage) {
+        const int n0 = reverse ? len - 32 - t0 : t0, valid = t_end - t0;
+        const long long at = ((long long)base + (long long)n0 * (long long)a.ts.sn) * T::ES;
+#pragma unroll
+        for (int i = 0; i < T::LOADS; ++i) {
+            const int k = i * T::WAVES + wave;
+            const char *src = static_cast<const char *>(a.in[job][k / T::TILE_LOADS]) + at;
+            const unsigned off = valid >= 32 ? offset[i] : offset_of(i, valid);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + off),
+                                             (__attribute__((address_space(3))) void *)(lds + stage * T::SET + k * 1024), 16, 0, 0);
+        }
+    };
+    const int chunks = t_begin < t_end ? (t_end - t_begin + 31) / 32 : 0;
+#pragma unroll
+    for (int i = 0; i < T::STAGES - 1; ++i)
+        if (i < chunks) load(t_begin + 32 * i, i);
+
+    // the state before the segment: column 32 part + l32
     f32x16 acc[CT];
-    const int col = 32 * wave + l32;
+    const int col = 32 * part + l32;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc[ct] = splat16(0.f);
-    if constexpr (!SUM) {
-        const bool from_slot = a.segments > 1;
-        const float *s = from_slot ? a.slots + slot : job.first ? job.first + (size_t)bh * (D * D) : nullptr;
+    const size_t slot = (((size_t)job * a.BH + bh) * a.segments + seg) * (D * D);
+    if constexpr (KIND != SUM) {
+        const float *s = a.segments > 1 ? a.slots + slot : role.first ? role.first + (size_t)bh * (D * D) : nullptr;
         if (s && col < D) {
-            const bool turned = !from_slot && job.first_turned;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int row = 32 * ct + perm_index(r >> 3, hh, r & 7);
-                    if (D >= 32 || row < D) acc[ct][r] = turned ? s[(size_t)col * D + row] : s[(size_t)row * D + col];
+                    const int row = state_row(ct, r, hh);
+                    if (D >= 32 || row < D) acc[ct][r] = role.turned ? s[(size_t)col * D + row] : s[(size_t)row * D + col];
                 }
         }
     }
 
     // weights, as far as they are the same in every chunk
     float wp[16], wi = 0.f, wu[16];
-    if constexpr (!SUM) {
+    if constexpr (KIND != SUM) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int gap = l32 - perm_index(r >> 3, hh, r & 7);
-            wp[r] = gap >= 0 ? job.p * fast_exp2(e2 * gap) : 0.f;
+            wp[r] = gap >= 0 ? a.p * fast_exp2(e2 * gap) : 0.f;
         }
-        wi = job.w * fast_exp2(e2 * (l32 + lead));
+        wi = a.w * fast_exp2(e2 * (l32 + lead));
     }
-    const auto update_weights = [&](int n) {
+    const auto update_weights = [&](int n) {       // (a token behind the end weighs nothing)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) wu[r] = job.m * fast_exp2(e2 * max(n - lead - perm_index(r >> 3, hh, r & 7), 0));
+        for (int r = 0; r < 16; ++r) {
+            const int u = perm_index(r >> 3, hh, r & 7);
+            wu[r] = u < n ? a.m[job] * fast_exp2(e2 * (n - lead - u)) : 0.f;
+        }
     };
     update_weights(32);
-    float fade = fast_exp2(e2 * 32.f);
+    Fade fade(g, 32);
     int e_state = 0, e_p = 0, e_z = 0;    // fp16: of the state as an operand, of P, of the weighted z (the accumulators hold C 2^-e_z)
 
-    if constexpr (D < 32) {       // the columns that no load ever writes
-        for (int q = tid; q < T::BUFFERS * 3 * T::BYTES / 16; q += T::THREADS) reinterpret_cast<u32x4 *>(lds)[q] = u32x4{0, 0, 0, 0};
-        __syncthreads();
-    }
+    // tiles of this wave's role
+    constexpr int X = KIND == FORWARD ? 0 : -1, Y = KIND == SUM ? 0 : KIND == FORWARD ? 1 : -1, Z = KIND == SUM ? 1 : KIND == FORWARD ? 2 : -1;
+    const int x_at = (KIND == DKDV ? (which ? 1 : 2) : X) * T::BYTES, y_at = (KIND == DKDV ? (which ? 0 : 3) : Y) * T::BYTES,
+              z_at = (KIND == DKDV ? (which ? 3 : 0) : Z) * T::BYTES;
 
-    u32x4 px[SUM ? 1 : T::PIECES], py[T::PIECES], pz[T::PIECES];
-    const auto load = [&](int t0) {
-#pragma unroll
-        for (int i = 0; i < T::PIECES; ++i) {
-            const int q = tid + i * T::THREADS, t = t0 + q / T::ROW_PIECES;
-            const int tc = min(t, t_end - 1);
-            const size_t off = (base + tok_off(a.ts, reverse ? len - 1 - tc : tc)) * T::ES + q % T::ROW_PIECES * 16;
-            if constexpr (!SUM) px[i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(job.x) + off);
-            py[i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(job.y) + off);
-            pz[i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(job.z) + off);
-            if (t >= t_end) {
-                if constexpr (!SUM) px[i] = u32x4{0, 0, 0, 0};
-                py[i] = u32x4{0, 0, 0, 0};
-                pz[i] = u32x4{0, 0, 0, 0};
-            }
-        }
-    };
-    if (t_begin < t_end) load(t_begin);
-    int buf = 0;
-    for (int t0 = t_begin; t0 < t_end; t0 += 32) {
-        char *const tx = lds + buf * 3 * T::BYTES, *const ty = tx + T::BYTES, *const tz = ty + T::BYTES;
-        if constexpr (T::BUFFERS == 1) __syncthreads();
-#pragma unroll
-        for (int i = 0; i < T::PIECES; ++i) {
-            const int q = tid + i * T::THREADS, at = q / T::ROW_PIECES * T::ROW + q % T::ROW_PIECES * 16;
-            if constexpr (!SUM) *reinterpret_cast<u32x4 *>(tx + at) = px[i];
-            *reinterpret_cast<u32x4 *>(ty + at) = py[i];
-            *reinterpret_cast<u32x4 *>(tz + at) = pz[i];
-        }
-        __syncthreads();
-        if (t0 + 32 < t_end) load(t0 + 32);
-        if (t0 + 32 > t_end) {
-            update_weights(t_end - t0);
-            fade = fast_exp2(e2 * (t_end - t0));
+    int stage = 0;
+    for (int i = 0; i < chunks; ++i) {
+        const int t0 = t_begin + 32 * i;
+        // This wave's part of chunk i is there when no more is on its way than what was asked for behind it: the loads of
+        // STAGES - 2 chunks, and the stores of the chunks since (full ones; the barrier makes it everyone's part).  Its own reads
+        // of chunk i - 1 have returned.
+        if (i + T::STAGES - 1 > chunks) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        else if (i < T::STAGES - 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::STAGES - 2) * T::LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::STAGES - 2) * T::LOADS + (T::STAGES - 1) * T::STORES) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // (everyone is done with chunk i - 1, whose place this takes)
+        if (i + T::STAGES - 1 < chunks) load(t0 + 32 * (T::STAGES - 1), stage == 0 ? T::STAGES - 1 : stage - 1);
+        const char *const set = lds + stage * T::SET;
+        const char *const tx = set + x_at, *const ty = set + y_at, *const tz = set + z_at;
+        const int valid = t_end - t0;
+        float faded = fade.next();
+        if (valid < 32) {
+            update_weights(valid);
+            faded = fast_exp2(e2 * valid);
         }
 
-        const Frag<DT> zc[2] = {col_frag<DT, D>(tz, wave, 0, lane), col_frag<DT, D>(tz, wave, 1, lane)};
-        if constexpr (!SUM) {
+        const Frag<DT> zc[2] = {col_frag<DT, D, false>(tz, part, 0, lane), col_frag<DT, D, false>(tz, part, 1, lane)};
+        if constexpr (KIND != SUM) {
             float scale_state = 1.f;
             if constexpr (F16) {
                 float largest = 0.f;
@@ -297,25 +380,36 @@ __global__ __launch_bounds__((Tile<DT, D>::THREADS), 2) void decay_scan_kernel(c
             }
             const int t = t0 + l32;
             if (t < t_end) {
-                char *const row = static_cast<char *>(job.out) +
-                                  (base + tok_off(a.ts, reverse ? len - 1 - t : t) + 32 * wave) * T::ES;
+                char *const row = static_cast<char *>(role.out) +
+                                  (base + tok_off(a.ts, reverse ? len - 1 - t : t) + 32 * part) * T::ES;
+                if constexpr (F16) {
 #pragma unroll
-                for (int g = 0; g < (D < 32 ? 2 : 4); ++g) {
-                    float v[4];
+                    for (int r = 0; r < 16; ++r) o[r] *= scale_out;
+                }
+                if constexpr (DT == FLARE_F32) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = F16 ? o[4 * g + e] * scale_out : o[4 * g + e];
-                    if constexpr (DT == FLARE_F32) {
-                        *reinterpret_cast<float4 *>(row + (8 * g + 4 * hh) * 4) = make_float4(v[0], v[1], v[2], v[3]);
-                    } else {
-                        u32x2 w;
-                        w[0] = pack_elems<F16>(v[0], v[1]);
-                        w[1] = pack_elems<F16>(v[2], v[3]);
-                        *reinterpret_cast<u32x2 *>(row + (8 * g + 4 * hh) * 2) = w;
+                    for (int q = 0; q < (D < 32 ? 2 : 4); ++q)
+                        *reinterpret_cast<float4 *>(row + (8 * q + 4 * hh) * 4) =
+                            make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                } else {
+                    // register group q holds columns 8 q + 4 hh + 0..3: the halves of the wave trade groups, for 16 bytes a lane
+#pragma unroll
+                    for (int q = 0; q < (D < 32 ? 1 : 2); ++q) {
+                        u32x4 w;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const auto both = __builtin_amdgcn_permlane32_swap(pack_elems<F16>(o[8 * q + 2 * k], o[8 * q + 2 * k + 1]),
+                                                                               pack_elems<F16>(o[8 * q + 4 + 2 * k], o[8 * q + 5 + 2 * k]),
+                                                                               false, false);
+                            w[k] = both[0];
+                            w[2 + k] = both[1];
+                        }
+                        *reinterpret_cast<u32x4 *>(row + (16 * q + 8 * hh) * 2) = w;
                     }
                 }
             }
         }
-        float weighted[16], fade_acc = fade;
+        float weighted[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) weighted[r] = elem_of<DT>(zc[r >> 3], r & 7) * wu[r];
         if constexpr (F16) {
@@ -324,7 +418,7 @@ __global__ __launch_bounds__((Tile<DT, D>::THREADS), 2) void decay_scan_kernel(c
             for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(weighted[r]));
             const int before = e_z;
             fit_exponent(e_z, largest);
-            fade_acc = ldexpf(fade, before - e_z);
+            faded = ldexpf(faded, before - e_z);
             const float down = ldexpf(1.f, -e_z);
 #pragma unroll
             for (int r = 0; r < 16; ++r) weighted[r] *= down;
@@ -332,58 +426,65 @@ __global__ __launch_bounds__((Tile<DT, D>::THREADS), 2) void decay_scan_kernel(c
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[ct][r] *= fade_acc;
+            for (int r = 0; r < 16; ++r) acc[ct][r] *= faded;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             float left[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) left[e] = weighted[8 * ks + e];
-            Frag<DT> plane[T::PLANES];
+            Frag<DT> plane[PLANES];
 #pragma unroll
-            for (int k = 0; k < T::PLANES; ++k) {
+            for (int k = 0; k < PLANES; ++k) {
                 plane[k] = pack8<DT>(left);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) left[e] -= elem_of<DT>(plane[k], e);
             }
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                const Frag<DT> yc = col_frag<DT, D>(ty, ct, ks, lane);
+                const Frag<DT> yc = col_frag<DT, D, true>(ty, ct, ks, lane);
 #pragma unroll
-                for (int k = 0; k < T::PLANES; ++k) acc[ct] = mma<DT>(yc, plane[k], acc[ct]);
+                for (int k = 0; k < PLANES; ++k) acc[ct] = mma<DT>(yc, plane[k], acc[ct]);
             }
         }
-        if constexpr (T::BUFFERS == 2) buf ^= 1;
+        stage = stage + 1 == T::STAGES ? 0 : stage + 1;
     }
 
     float *dst = nullptr;
-    if constexpr (SUM) dst = a.slots + slot;
-    else if (job.last && t_begin + a.seg_len >= len) dst = job.last + (size_t)bh * (D * D);
+    if constexpr (KIND == SUM) dst = a.slots + slot;
+    else if (role.last && t_begin + a.seg_len >= len) dst = role.last + (size_t)bh * (D * D);
     if (dst && col < D) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int row = 32 * ct + perm_index(r >> 3, hh, r & 7);
+                const int row = state_row(ct, r, hh);
                 if (D >= 32 || row < D) dst[(size_t)row * D + col] = F16 ? ldexpf(acc[ct][r], e_z) : acc[ct][r];
             }
     }
 }
 
 // Segments' sums -> the state before each segment, in place: thread = four neighbouring entries of a state.
-__global__ __launch_bounds__(256) void decay_carry_kernel(const ScanArgs a, int d)
+struct CarryArgs {
+    const float *first[2];   // state before the first token of either job, or NULL
+    int turned[2];
+    const float *log_decay;
+    const int *lengths;
+    float *slots;
+    int H, N, BH, segments, seg_len, d;
+};
+__global__ __launch_bounds__(256) void decay_carry_kernel(const CarryArgs a)
 {
-    const int dd = d * d, tiles = (dd / 4 + 255) / 256;
+    const int d = a.d, dd = d * d, tiles = (dd / 4 + 255) / 256;
     const int i = 4 * (blockIdx.x % tiles * 256 + threadIdx.x), jbh = blockIdx.x / tiles;
     if (i >= dd) return;
     const int bh = jbh % a.BH, jb = jbh / a.BH;
-    const ScanJob &job = a.job[jb];
     const int len = item_length(a.lengths, bh / a.H, a.N);
     const int used = (len + a.seg_len - 1) / a.seg_len;
-    const float fade = fast_exp2(decay_log2(a.log_decay[bh % a.H]) * (float)a.seg_len);
+    Fade fade(a.log_decay[bh % a.H], a.seg_len);
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (job.first) {
-        const float *f = job.first + (size_t)bh * dd;
-        if (job.first_turned) {
+    if (a.first[jb]) {
+        const float *f = a.first[jb] + (size_t)bh * dd;
+        if (a.turned[jb]) {
             const int row = i / d, col = i % d;
             s = make_float4(f[(size_t)col * d + row], f[(size_t)(col + 1) * d + row], f[(size_t)(col + 2) * d + row],
                             f[(size_t)(col + 3) * d + row]);
@@ -396,7 +497,8 @@ __global__ __launch_bounds__(256) void decay_carry_kernel(const ScanArgs a, int 
         float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
         if (g + 1 < used) u = *reinterpret_cast<const float4 *>(slot);
         *reinterpret_cast<float4 *>(slot) = s;
-        s = make_float4(fmaf(s.x, fade, u.x), fmaf(s.y, fade, u.y), fmaf(s.z, fade, u.z), fmaf(s.w, fade, u.w));
+        const float f = fade.next();
+        s = make_float4(fmaf(s.x, f, u.x), fmaf(s.y, f, u.y), fmaf(s.z, f, u.z), fmaf(s.w, f, u.w));
     }
 }
 
@@ -469,10 +571,11 @@ TokStride decay_stride(const flare_decay_shape &s)
     if (s.layout == FLARE_BNHD) return TokStride{N * H * d, d, H * d, 0};
     return TokStride{H * N * d, N * d, d, 0};
 }
+// How the tokens are cut.  The slots of a forward pass are one job's, of a backward pass two (S and its gradient).
 struct DecayPlan { int segments, seg_len; };
-DecayPlan decay_plan(const flare_decay_shape &s, int jobs)
+DecayPlan decay_plan(const flare_decay_shape &s, bool backward)
 {
-    const long long waves = (s.d < 32 ? 1 : s.d / 32) * (long long)s.B * s.H * jobs;
+    const long long waves = (s.d < 32 ? 1 : s.d / 32) * (long long)s.B * s.H;
     long long want = (2048 + waves - 1) / waves;
     const long long most = (s.N + 255) / 256;
     if (want > most) want = most;
@@ -480,56 +583,155 @@ DecayPlan decay_plan(const flare_decay_shape &s, int jobs)
     const long long len = ((s.N + want - 1) / want + 31) / 32 * 32;
     return DecayPlan{(int)((s.N + len - 1) / len), (int)len};
 }
-size_t slot_bytes(const flare_decay_shape &s, int jobs)
+size_t slot_bytes(const flare_decay_shape &s, bool backward)
 {
-    const DecayPlan p = decay_plan(s, jobs);
-    return p.segments > 1 ? (size_t)jobs * s.B * s.H * p.segments * s.d * s.d * 4 : 0;
+    const DecayPlan p = decay_plan(s, backward);
+    return p.segments > 1 ? (size_t)(backward ? 2 : 1) * s.B * s.H * p.segments * s.d * s.d * 4 : 0;
 }
 
-template <int DT, int D>
-int run_scan(const flare_decay_shape &s, ScanArgs &a, int jobs, int kid, hipStream_t stream)
+// What the host knows of a call, whatever its type and d.
+struct DecayCall {
+    const flare_decay_shape *s;
+    const void *q, *k, *v, *d_o;
+    const float *log_decay;
+    const int *lengths;
+    const float *state_in, *dstate_out;
+    void *o, *dq, *dk, *dv;
+    float *state_out, *dstate_in;
+    float scale;
+    float *slots;
+    hipStream_t stream;
+};
+ScanArgs scan_args(const DecayCall &c, const DecayPlan &p)
 {
-    const dim3 grid((unsigned)(a.BH * (long long)a.segments), jobs);
-    if (a.segments > 1) {
-        {
-            LaunchTimer timer(KID_DECAY_SUM, stream);
-            decay_scan_kernel<DT, D, true><<<grid, Tile<DT, D>::THREADS, 0, stream>>>(a);
-        }
-        LaunchTimer timer(KID_DECAY_CARRY, stream);
-        decay_carry_kernel<<<(D * D / 4 + 255) / 256 * a.BH * jobs, 256, 0, stream>>>(a, D);
-    }
-    LaunchTimer timer(kid, stream);
-    decay_scan_kernel<DT, D, false><<<grid, Tile<DT, D>::THREADS, 0, stream>>>(a);
-    return check_launch();
+    ScanArgs a{};
+    a.log_decay = c.log_decay;
+    a.lengths = c.lengths;
+    a.slots = c.slots;
+    a.ts = decay_stride(*c.s);
+    a.H = c.s->H;
+    a.N = c.s->N;
+    a.BH = c.s->B * c.s->H;
+    a.segments = p.segments;
+    a.seg_len = p.seg_len;
+    return a;
 }
-template <int DT>
-int run_scan_d(const flare_decay_shape &s, ScanArgs &a, int jobs, int kid, hipStream_t stream)
+template <int DT, int D, int KIND>
+void launch_scan(const ScanArgs &a, int jobs, bool exact, int kid, hipStream_t stream)
 {
-    switch (s.d) {
-        case 16: return run_scan<DT, 16>(s, a, jobs, kid, stream);
-        case 32: return run_scan<DT, 32>(s, a, jobs, kid, stream);
-        case 64: return run_scan<DT, 64>(s, a, jobs, kid, stream);
-        case 128: return run_scan<DT, 128>(s, a, jobs, kid, stream);
+    const dim3 grid((unsigned)((a.BH * (long long)a.segments + 7) / 8 * 8), jobs);
+    LaunchTimer timer(kid, stream);
+    if (exact && DT == FLARE_BF16)       // (the other types make no difference)
+        decay_scan_kernel<DT, D, KIND, DT == FLARE_BF16><<<grid, Scan<DT, D, KIND>::THREADS, 0, stream>>>(a);
+    else
+        decay_scan_kernel<DT, D, KIND, false><<<grid, Scan<DT, D, KIND>::THREADS, 0, stream>>>(a);
+}
+void launch_carry(const DecayCall &c, const DecayPlan &p, int jobs, const float *first0, int turned0, const float *first1)
+{
+    CarryArgs a{};
+    a.first[0] = first0;
+    a.first[1] = first1;
+    a.turned[0] = turned0;
+    a.log_decay = c.log_decay;
+    a.lengths = c.lengths;
+    a.slots = c.slots;
+    a.H = c.s->H;
+    a.N = c.s->N;
+    a.BH = c.s->B * c.s->H;
+    a.segments = p.segments;
+    a.seg_len = p.seg_len;
+    a.d = c.s->d;
+    LaunchTimer timer(KID_DECAY_CARRY, c.stream);
+    decay_carry_kernel<<<(a.d * a.d / 4 + 255) / 256 * a.BH * jobs, 256, 0, c.stream>>>(a);
+}
+
+struct ForwardPass {
+    template <int DT, int D>
+    static int run(const DecayCall &c)
+    {
+        const DecayPlan p = decay_plan(*c.s, false);
+        const bool exact = c.state_out != nullptr;
+        if (p.segments > 1) {
+            ScanArgs a = scan_args(c, p);
+            a.in[0][0] = c.k;
+            a.in[0][1] = c.v;
+            a.m[0] = 1.f;
+            launch_scan<DT, D, SUM>(a, 1, exact, KID_DECAY_SUM, c.stream);
+            launch_carry(c, p, 1, c.state_in, 0, nullptr);
+        }
+        ScanArgs a = scan_args(c, p);
+        a.in[0][0] = c.q;
+        a.in[0][1] = c.k;
+        a.in[0][2] = c.v;
+        a.role[0] = Role{c.o, c.state_in, c.state_out, 0};
+        a.p = a.w = c.scale;
+        a.m[0] = 1.f;
+        launch_scan<DT, D, FORWARD>(a, 1, exact, KID_DECAY_FORWARD, c.stream);
+        return check_launch();
+    }
+};
+struct BackwardPass {
+    template <int DT, int D>
+    static int run(const DecayCall &c)
+    {
+        const DecayPlan p = decay_plan(*c.s, true);
+        const bool exact = c.dstate_in != nullptr;
+        if (p.segments > 1) {
+            // job 0: the transposed S (rows by v), forwards; job 1: its gradient (rows by q), backwards
+            ScanArgs a = scan_args(c, p);
+            a.in[0][0] = c.v;
+            a.in[0][1] = c.k;
+            a.in[1][0] = c.q;
+            a.in[1][1] = c.d_o;
+            a.m[0] = 1.f;
+            a.m[1] = c.scale;
+            a.reverse[1] = 1;
+            launch_scan<DT, D, SUM>(a, 2, exact, KID_DECAY_SUM, c.stream);
+            launch_carry(c, p, 2, c.state_in, 1, c.dstate_out);
+        }
+        const bool slots = p.segments > 1;
+        ScanArgs a = scan_args(c, p);
+        a.in[0][0] = c.d_o;
+        a.in[0][1] = c.v;
+        a.in[0][2] = c.k;
+        a.role[0] = Role{c.dq, c.state_in, nullptr, slots ? 0 : 1};
+        a.p = a.w = c.scale;
+        a.m[0] = 1.f;
+        launch_scan<DT, D, FORWARD>(a, 1, false, KID_DECAY_DQ, c.stream);
+        a = scan_args(c, p);
+        a.in[0][0] = c.q;
+        a.in[0][1] = c.k;
+        a.in[0][2] = c.v;
+        a.in[0][3] = c.d_o;
+        a.role[0] = Role{c.dk, c.dstate_out, nullptr, 1};            // x = v, y = dO, z = q
+        a.role[1] = Role{c.dv, c.dstate_out, c.dstate_in, 0};        // x = k, y = q, z = dO
+        a.p = c.scale;
+        a.w = 1.f;
+        a.m[0] = c.scale;
+        a.reverse[0] = 1;
+        if (slots) a.slots += (size_t)a.BH * p.segments * D * D;
+        launch_scan<DT, D, DKDV>(a, 1, exact, KID_DECAY_DKDV, c.stream);
+        return check_launch();
+    }
+};
+template <typename Pass, int DT>
+int run_pass_d(const DecayCall &c)
+{
+    switch (c.s->d) {
+        case 16: return Pass::template run<DT, 16>(c);
+        case 32: return Pass::template run<DT, 32>(c);
+        case 64: return Pass::template run<DT, 64>(c);
+        case 128: return Pass::template run<DT, 128>(c);
         default: return FLARE_EUNSUPPORTED;
     }
 }
-int run_scan_any(const flare_decay_shape &s, ScanArgs &a, int jobs, int kid, const float *log_decay, const int *lengths, void *ws,
-                 hipStream_t stream)
+template <typename Pass>
+int run_pass(const DecayCall &c)
 {
-    const DecayPlan p = decay_plan(s, jobs);
-    a.log_decay = log_decay;
-    a.lengths = lengths;
-    a.slots = static_cast<float *>(ws);
-    a.ts = decay_stride(s);
-    a.H = s.H;
-    a.N = s.N;
-    a.BH = s.B * s.H;
-    a.segments = p.segments;
-    a.seg_len = p.seg_len;
-    switch (s.dtype) {
-        case FLARE_F32: return run_scan_d<FLARE_F32>(s, a, jobs, kid, stream);
-        case FLARE_BF16: return run_scan_d<FLARE_BF16>(s, a, jobs, kid, stream);
-        default: return run_scan_d<FLARE_F16>(s, a, jobs, kid, stream);
+    switch (c.s->dtype) {
+        case FLARE_F32: return run_pass_d<Pass, FLARE_F32>(c);
+        case FLARE_BF16: return run_pass_d<Pass, FLARE_BF16>(c);
+        default: return run_pass_d<Pass, FLARE_F16>(c);
     }
 }
 
@@ -562,27 +764,51 @@ int run_step_d(const flare_decay_shape &s, const void *q, const void *k, const v
 
 }  // namespace
 
-size_t decay_fwd_bytes(const flare_decay_shape &s) { return slot_bytes(s, 1); }
-size_t decay_bwd_bytes(const flare_decay_shape &s) { return slot_bytes(s, 3); }
+size_t decay_fwd_bytes(const flare_decay_shape &s) { return slot_bytes(s, false); }
+size_t decay_bwd_bytes(const flare_decay_shape &s) { return slot_bytes(s, true); }
 
 int decay_forward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
                   const int *lengths, const float *state_in, void *o, float *state_out, float scale, void *ws,
                   hipStream_t stream)
 {
-    ScanArgs a{};
-    a.job[0] = ScanJob{q, k, v, o, state_in, state_out, scale, scale, 1.f, 0, 0};
-    return run_scan_any(s, a, 1, KID_DECAY_FORWARD, log_decay, lengths, ws, stream);
+    DecayCall c{};
+    c.s = &s;
+    c.q = q;
+    c.k = k;
+    c.v = v;
+    c.log_decay = log_decay;
+    c.lengths = lengths;
+    c.state_in = state_in;
+    c.o = o;
+    c.state_out = state_out;
+    c.scale = scale;
+    c.slots = static_cast<float *>(ws);
+    c.stream = stream;
+    return run_pass<ForwardPass>(c);
 }
 
 int decay_backward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
                    const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq, void *dk,
                    void *dv, float *dstate_in, float scale, void *ws, hipStream_t stream)
 {
-    ScanArgs a{};
-    a.job[0] = ScanJob{d_o, v, k, dq, state_in, nullptr, scale, scale, 1.f, 0, 1};
-    a.job[1] = ScanJob{v, d_o, q, dk, dstate_out, nullptr, scale, 1.f, scale, 1, 1};
-    a.job[2] = ScanJob{k, q, d_o, dv, dstate_out, dstate_in, scale, 1.f, scale, 1, 0};
-    return run_scan_any(s, a, 3, KID_DECAY_BACKWARD, log_decay, lengths, ws, stream);
+    DecayCall c{};
+    c.s = &s;
+    c.q = q;
+    c.k = k;
+    c.v = v;
+    c.d_o = d_o;
+    c.log_decay = log_decay;
+    c.lengths = lengths;
+    c.state_in = state_in;
+    c.dstate_out = dstate_out;
+    c.dq = dq;
+    c.dk = dk;
+    c.dv = dv;
+    c.dstate_in = dstate_in;
+    c.scale = scale;
+    c.slots = static_cast<float *>(ws);
+    c.stream = stream;
+    return run_pass<BackwardPass>(c);
 }
 
 int decay_step(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay, const int *active,

@@ -33,7 +33,8 @@ enum KernelId {
     KID_DECAY_SUM,
     KID_DECAY_CARRY,
     KID_DECAY_FORWARD,
-    KID_DECAY_BACKWARD,
+    KID_DECAY_DQ,
+    KID_DECAY_DKDV,
     KID_DECAY_STEP,
     KID_NORM_FORWARD,
     KID_NORM_BACKWARD,
