@@ -286,29 +286,32 @@ typedef struct {
     flare_layout layout;
 } flare_decay_shape;
 
-/* Scratch bytes of flare_decay_forward and flare_decay_backward (either pointer may be NULL); may be 0.  Host-only. */
-int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes);
+/* Scratch bytes of flare_decay_forward and flare_decay_backward without marks (with them never more; the forward then
+ * needs none), and the size of marks; each pointer may be NULL, each number 0.  Host-only. */
+int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes, size_t *marks_bytes);
 
 /*
  *   q, k, v, log_decay, lengths (or NULL), state_in (or NULL: zero)                                       (in)
  *   o: q's shape and dtype; state_out (or NULL)                                                           (out)
+ *   marks (or NULL): states along the sequences, which save the backward a pass over k and v             (out)
  * o may be the buffer of q, k or v, and state_out that of state_in.
  */
 int flare_decay_forward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
-                        const int *lengths, const float *state_in, void *o, float *state_out, float scale,
+                        const int *lengths, const float *state_in, void *o, float *state_out, float *marks, float scale,
                         void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Backward.  With G_t the gradient of S_{t-1} (G behind the last token = dstate_out, or zero):
  *     dS_t = scale q_t d_o_t^T + G_{t+1},  G_t = l dS_t,  dq_t = scale S_t d_o_t,  dk_t = dS_t v_t,  dv_t = dS_t^T k_t
- *   q, k, v, log_decay, lengths, state_in as in the forward; d_o: o's gradient; dstate_out (or NULL: zero)  (in)
+ *   q, k, v, log_decay, lengths, state_in as in the forward; marks: what it wrote, or NULL                (in)
+ *   d_o: o's gradient; dstate_out (or NULL: zero): state_out's                                            (in)
  *   dq, dk, dv: q's shape and dtype; dstate_in (or NULL)                                                  (out)
  * No output may overlap an input.
  */
 int flare_decay_backward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
-                         const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq,
-                         void *dk, void *dv, float *dstate_in, float scale, void *workspace, size_t workspace_bytes,
-                         void *stream);
+                         const int *lengths, const float *state_in, const float *marks, const void *d_o,
+                         const float *dstate_out, void *dq, void *dk, void *dv, float *dstate_in, float scale,
+                         void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * One token of each item: shape->N is 1 (else FLARE_EINVAL); q, k, v, o are [B][H][d].

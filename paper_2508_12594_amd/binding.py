@@ -90,9 +90,9 @@ def load():
     lib.flare_spectral.argtypes = [sp, vp, vp, fp, fp, ctypes.c_float, ctypes.c_int, fp, fp, fp, vp, ctypes.c_size_t, vp]
     size, dp, np = ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(DecayShape), ctypes.POINTER(NormShape)
     pp, f = ctypes.POINTER(NormParams), ctypes.c_float
-    lib.flare_decay_workspace_bytes.argtypes = [dp, size, size]
-    lib.flare_decay_forward.argtypes = [dp, vp, vp, vp, fp, vp, fp, vp, fp, f, vp, ctypes.c_size_t, vp]
-    lib.flare_decay_backward.argtypes = [dp, vp, vp, vp, fp, vp, fp, vp, fp, vp, vp, vp, fp, f, vp, ctypes.c_size_t, vp]
+    lib.flare_decay_workspace_bytes.argtypes = [dp, size, size, size]
+    lib.flare_decay_forward.argtypes = [dp, vp, vp, vp, fp, vp, fp, vp, fp, fp, f, vp, ctypes.c_size_t, vp]
+    lib.flare_decay_backward.argtypes = [dp, vp, vp, vp, fp, vp, fp, fp, vp, fp, vp, vp, vp, fp, f, vp, ctypes.c_size_t, vp]
     lib.flare_decay_step.argtypes = [dp, vp, vp, vp, fp, vp, fp, fp, vp, f, vp]
     lib.flare_residual_norm_workspace_bytes.argtypes = [np, size]
     lib.flare_residual_norm_forward.argtypes = [np, pp, vp, vp, vp, vp, vp, fp, f, f, vp]
@@ -286,31 +286,33 @@ def spectral(q_lat, k, lse_enc, lse_dec, scale, first=0, want_gram=False, stream
 
 # ---- decay mixer -----------------------------------------------------------------------------------------------------
 def decay_workspace_bytes(B, H, N, d, dtype_code, layout="bhnd"):
-    """(forward bytes, backward bytes) of scratch of the decay mixer for this shape; may be 0."""
+    """(forward bytes, backward bytes, bytes of marks) of the decay mixer for this shape; each may be 0."""
     shp = DecayShape(B, H, N, d, dtype_code, _layout(layout))
-    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    _check(load().flare_decay_workspace_bytes(ctypes.byref(shp), ctypes.byref(f), ctypes.byref(b)),
+    f, b, m = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(load().flare_decay_workspace_bytes(ctypes.byref(shp), ctypes.byref(f), ctypes.byref(b), ctypes.byref(m)),
            "flare_decay_workspace_bytes")
-    return int(f.value), int(b.value)
+    return int(f.value), int(b.value), int(m.value)
 
 
 def decay_forward(q, k, v, log_decay, scale, lengths=None, state=None, o=None, state_out=None, want_state=False,
-                  workspace=None, stream=None, layout="bhnd"):
+                  marks=None, workspace=None, stream=None, layout="bhnd"):
     """flare_decay_forward: causal linear attention with a decay for each head; returns (o, state_out).
 
     layout 'bhnd': q, k, v, o are [B,H,N,d]; 'bnhd': they are [B,N,H,d].  log_decay [H] fp32, at most 0.  lengths [B] int32:
     a padded batch.  state [B,H,d,d] fp32: what came before the first token.  state_out is written where it is given
-    (it may be `state`) or with want_state, and None otherwise."""
+    (it may be `state`) or with want_state, and None otherwise.  marks (fp32, of the size that decay_workspace_bytes
+    says) is filled when given, for the backward."""
     return (_ext or _native()).decay_forward(q, k, v, log_decay, scale, lengths, state, o, state_out, bool(want_state),
-                                             workspace, stream, _layout(layout))
+                                             marks, workspace, stream, _layout(layout))
 
 
 def decay_backward(q, k, v, log_decay, d_o, scale, lengths=None, state=None, dstate_out=None, dq=None, dk=None, dv=None,
-                   dstate=None, want_dstate=False, workspace=None, stream=None, layout="bhnd"):
+                   dstate=None, want_dstate=False, marks=None, workspace=None, stream=None, layout="bhnd"):
     """flare_decay_backward: returns (dq, dk, dv, dstate); dstate, the gradient of `state`, is written where it is given or
-    with want_dstate, and None otherwise.  dstate_out: the gradient of the forward's state_out."""
+    with want_dstate, and None otherwise.  dstate_out: the gradient of the forward's state_out.  marks: what the forward
+    left (saves a pass over k and v)."""
     return (_ext or _native()).decay_backward(q, k, v, log_decay, d_o, scale, lengths, state, dstate_out, dq, dk, dv, dstate,
-                                              bool(want_dstate), workspace, stream, _layout(layout))
+                                              bool(want_dstate), marks, workspace, stream, _layout(layout))
 
 
 def decay_step(q, k, v, log_decay, state, scale, state_out=None, active=None, o=None, stream=None):

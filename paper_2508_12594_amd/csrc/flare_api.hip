@@ -340,45 +340,46 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
                         static_cast<hipStream_t>(stream));
 }
 
-int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes)
+int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes, size_t *marks_bytes)
 {
     const int rc = check_decay(shape);
     if (rc != FLARE_OK) return rc;
-    if (fwd_bytes) *fwd_bytes = decay_fwd_bytes(*shape);
-    if (bwd_bytes) *bwd_bytes = decay_bwd_bytes(*shape);
+    if (fwd_bytes) *fwd_bytes = decay_fwd_bytes(*shape, false);
+    if (bwd_bytes) *bwd_bytes = decay_bwd_bytes(*shape, false);
+    if (marks_bytes) *marks_bytes = decay_marks_bytes(*shape);
     return FLARE_OK;
 }
 
 int flare_decay_forward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
-                        const int *lengths, const float *state_in, void *o, float *state_out, float scale, void *workspace,
-                        size_t workspace_bytes, void *stream)
+                        const int *lengths, const float *state_in, void *o, float *state_out, float *marks, float scale,
+                        void *workspace, size_t workspace_bytes, void *stream)
 {
     const int rc = check_decay(shape);
     if (rc != FLARE_OK) return rc;
     if (!q || !k || !v || !log_decay || !o) return FLARE_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(lengths) ||
-        !aligned16(state_in) || !aligned16(o) || !aligned16(state_out) || !aligned16(workspace))
+        !aligned16(state_in) || !aligned16(o) || !aligned16(state_out) || !aligned16(marks) || !aligned16(workspace))
         return FLARE_EALIGN;
-    const size_t need = decay_fwd_bytes(*shape);
+    const size_t need = decay_fwd_bytes(*shape, marks != nullptr);
     if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
-    return decay_forward(*shape, q, k, v, log_decay, lengths, state_in, o, state_out, scale, workspace,
+    return decay_forward(*shape, q, k, v, log_decay, lengths, state_in, o, state_out, marks, scale, workspace,
                          static_cast<hipStream_t>(stream));
 }
 
 int flare_decay_backward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
-                         const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq, void *dk,
-                         void *dv, float *dstate_in, float scale, void *workspace, size_t workspace_bytes, void *stream)
+                         const int *lengths, const float *state_in, const float *marks, const void *d_o,
+                         const float *dstate_out, void *dq, void *dk, void *dv, float *dstate_in, float scale, void *workspace, size_t workspace_bytes, void *stream)
 {
     const int rc = check_decay(shape);
     if (rc != FLARE_OK) return rc;
     if (!q || !k || !v || !log_decay || !d_o || !dq || !dk || !dv) return FLARE_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(lengths) ||
-        !aligned16(state_in) || !aligned16(d_o) || !aligned16(dstate_out) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
+        !aligned16(state_in) || !aligned16(marks) || !aligned16(d_o) || !aligned16(dstate_out) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
         !aligned16(dstate_in) || !aligned16(workspace))
         return FLARE_EALIGN;
-    const size_t need = decay_bwd_bytes(*shape);
+    const size_t need = decay_bwd_bytes(*shape, marks != nullptr);
     if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
-    return decay_backward(*shape, q, k, v, log_decay, lengths, state_in, d_o, dstate_out, dq, dk, dv, dstate_in, scale, workspace,
+    return decay_backward(*shape, q, k, v, log_decay, lengths, state_in, marks, d_o, dstate_out, dq, dk, dv, dstate_in, scale, workspace,
                           static_cast<hipStream_t>(stream));
 }
 

@@ -16,7 +16,7 @@
 //   O^T += Z^T P^T         likewise P^T's accumulators are the B operand: a contraction index in accumulator order
 //   C   += Y^T (weight Z)  Y and Z read down their columns (transposing LDS reads), Y's columns in the order that makes the
 //                          state's registers eight neighbouring rows (state_row)
-// so that nothing but the token tiles passes through LDS.  These come by direct loads into LDS, two or three chunks ahead.
+// so that nothing but the token tiles passes through LDS.  These come by direct loads into LDS, one to three chunks ahead.
 // dK and dV share their four tiles: a workgroup of theirs has waves in two roles.
 //
 // Where (b,h) are too few to fill the chip the tokens are cut into segments: a first pass takes each segment's own sum, a
@@ -73,16 +73,19 @@ struct Role {
     int turned;            // `first` and the slots hold the transposed state
 };
 struct ScanArgs {
-    const void *in[2][4];     // the tiles of either job (two jobs only where segments are summed)
+    const void *in[4];        // the tiles
     Role role[2];
-    float p, w, m[2];         // see above; m of either job
-    int reverse[2];           // tokens from the last to the first (then lead = 0)
+    float p, w, m;            // see above
+    int reverse;              // tokens from the last to the first (then lead = 0)
+    int whole;                // (sums) of the last segment too: the state behind it is asked for
     const float *log_decay;   // [H]
     const int *lengths;       // [B] or NULL
-    float *slots;             // [job][B*H][segments][d][d]: a segment's own sum, then the state before it
+    float *slots;             // [B*H][segments][d][d]: a segment's own sum, then the state before it
     TokStride ts;
     int H, N, BH, segments, seg_len;
 };
+
+constexpr float kSlow = 0x1p-16f;
 
 // SUM: a segment's own sum (tiles y, z); FORWARD: one role (x, y, z), also dQ; DKDV: two (q, k, v, dO).
 enum ScanKind { SUM = 0, FORWARD = 1, DKDV = 2 };
@@ -97,10 +100,13 @@ struct Scan {
     static constexpr int PIECES = ROW / 16;                        // of a row
     static constexpr int TILE_LOADS = BYTES / 1024;                // wave-wide loads of a tile; those of all tiles go round the waves
     static constexpr int LOADS = TILES * TILE_LOADS / WAVES;       // and so many of them are each wave's
-    // Chunks held in LDS: as many as leave room for eight waves on a CU, two at least, four at most.
+    // Chunks held in LDS: as many as leave room for eight waves on a CU, at most four (the sums, which have least to do with a
+    // chunk; dK and dV, whose workgroup is alone on its CU).  Scans of three tiles need no more than two: 119 us, 122 with three
+    // (16 heads, 32768 tokens, d = 128).
     static constexpr int FIT = 160 * 1024 / (SET * (WAVES < 8 ? 8 / WAVES : 1));
-    static constexpr int STAGES = FIT < 2 ? 2 : FIT > 4 ? 4 : FIT;
-    static constexpr int STORES = KIND == SUM ? 0 : (D < 32 ? 1 : 2) * (ES / 2);   // of a wave, each full chunk
+    static constexpr int STAGES = FIT <= 2 || KIND == FORWARD ? 2 : FIT > 4 ? 4 : FIT;
+    static constexpr int STORES = (D < 32 ? 1 : 2) * (ES / 2);   // of a wave, each full chunk
+    static constexpr int GROUP = ROW >= 256 ? 1 : 256 / ROW;       // heads side by side in 256 bytes
     static constexpr int PER_SIMD = WAVES * (160 * 1024 / (STAGES * SET)) >= 8 ? 2 : 1;   // waves (fp32, d = 128: one)
     static_assert(TILES * TILE_LOADS % WAVES == 0 && STAGES * SET <= 160 * 1024, "");
 };
@@ -196,84 +202,240 @@ __device__ __forceinline__ Frag<DT> col_frag(const char *tile, int ct, int ks, i
 
 // fp16 operands made of fp32 values (the state, P, the weighted z) are scaled by a power of two that the whole wave shares, so
 // that the largest of them lies between 2^2 and 2^15: a sum of many tokens may exceed 65504, and products of small
-// gradients lie among the subnormals.  `e` is kept from chunk to chunk; returns with the exponent to take off.
-__device__ __forceinline__ void fit_exponent(int &e, float largest)
+// gradients lie among the subnormals.  The exponent is kept from chunk to chunk, and moves in steps of 12 (every step leads
+// into the 13 octaves, so that at most one direction is taken).
+constexpr int kExponentStep = 12;
+// 0 where `largest` (already scaled) is fit for fp16, else the step that its exponent has to take
+__device__ __forceinline__ int exponent_step(float largest, int e)
 {
-    const bool some = __any(largest > 0.f);
-    while (e < 96 && __any(ldexpf(largest, -e) > 32768.f)) e += 12;
-    while (some && e > -96 && !__any(ldexpf(largest, -e) > 4.f)) e -= 12;
+    if (e < 96 && __any(largest > 32768.f)) return kExponentStep;
+    if (e > -96 && !__any(largest > 4.f) && __any(largest > 0.f)) return -kExponentStep;
+    return 0;
+}
+// Scales v until it is fit; returns the factor it took.
+template <int N>
+__device__ __forceinline__ float fit_exponent(float (&v)[N], int &e)
+{
+    float took = 1.f;
+    for (;;) {
+        float largest = 0.f;
+#pragma unroll
+        for (int r = 0; r < N; ++r) largest = fmaxf(largest, fabsf(v[r]));
+        const int step = exponent_step(largest, e);
+        if (step == 0) return took;
+        e += step;
+        const float by = step > 0 ? 1.f / (1 << kExponentStep) : (float)(1 << kExponentStep);
+        took *= by;
+#pragma unroll
+        for (int r = 0; r < N; ++r) v[r] *= by;
+    }
 }
 
-// EXACT: the state is an output.  PLANES of the weighted z: what the state sums is then good to 2^-22 (fp16) or 2^-24 (bf16)
-// of a term; otherwise, as it only meets x rounded to 16 bits, to 2^-16 with bf16.
+// Which (b,h) and segment a workgroup has.  Workgroups go round the eight XCDs: neighbouring heads whose rows share lines
+// (with [B][N][H][d]) go to one.
+struct Work { int bh, seg; bool none; };
+template <int GROUP>
+__device__ __forceinline__ Work work_of(const ScanArgs &a)
+{
+    const int turn = blockIdx.x >> 3, work = (turn / GROUP * 8 + (blockIdx.x & 7)) * GROUP + turn % GROUP;
+    return Work{work % a.BH, work / a.BH, work >= a.BH * a.segments};
+}
+
+// Loads of a chunk of tokens: 16 bytes a lane, 1024 a wave, straight into LDS, the loads of all tiles going round the waves.
+template <typename T>
+struct Loader {
+    const ScanArgs &a;
+    long long base;          // element offset of the (b,h) slice
+    int len, t_end, wave, lane;
+    unsigned row_bytes, offset[T::LOADS];
+    __device__ __forceinline__ Loader(const ScanArgs &args, int bh, int length, int end, int w, int l)
+        : a(args), base((long long)tok_base(args.ts, bh, args.H)), len(length), t_end(end), wave(w), lane(l),
+          row_bytes((unsigned)args.ts.sn * T::ES)
+    {
+#pragma unroll
+        for (int i = 0; i < T::LOADS; ++i) offset[i] = offset_of(i, 32);
+    }
+    // of load i, from the chunk's first row in memory
+    __device__ __forceinline__ unsigned offset_of(int i, int valid) const
+    {
+        const int q = (i * T::WAVES + wave) % T::TILE_LOADS * 64 + lane, r = q / T::PIECES;
+        const int c = (q % T::PIECES) ^ swizzle<T::ROW>(r), rc = min(r, valid - 1);   // behind the end: the last row again
+        return (unsigned)(a.reverse ? 31 - rc : rc) * row_bytes + 16 * c;
+    }
+    __device__ __forceinline__ void load(int t0, char *set) const
+    {
+        const int n0 = a.reverse ? len - 32 - t0 : t0, valid = t_end - t0;
+        const long long at = (base + (long long)n0 * (long long)a.ts.sn) * T::ES;
+#pragma unroll
+        for (int i = 0; i < T::LOADS; ++i) {
+            const int k = i * T::WAVES + wave;
+            const char *src = static_cast<const char *>(a.in[k / T::TILE_LOADS]) + at;
+            const unsigned off = valid >= 32 ? offset[i] : offset_of(i, valid);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + off),
+                                             (__attribute__((address_space(3))) void *)(set + k * 1024), 16, 0, 0);
+        }
+    }
+};
+
+// The bf16 (fp16) planes of 8 fp32 values: their sum is the value but for 2^-8 (2^-11) to the power of their number.
+template <int DT, int PLANES>
+__device__ __forceinline__ void split_planes(const float *x, Frag<DT> (&plane)[PLANES])
+{
+    float left[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) left[e] = x[e];
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k) {
+        plane[k] = pack8<DT>(left);
+        if (k + 1 < PLANES) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) left[e] -= elem_of<DT>(plane[k], e);
+        }
+    }
+}
+template <int DT, bool EXACT>
+constexpr int planes() { return DT == FLARE_F32 ? 1 : DT == FLARE_BF16 && EXACT ? 3 : 2; }
+
+// A segment's own sum, into its slot: sum_u l^(n-u-lead) y_u z_u^T.  From the segment's last chunk to its first, so that its
+// first tokens are the last to be read before the scan reads them again (256 MB of memory-side cache), and nothing has to be
+// multiplied but the weights.  EXACT: the state behind the sequence is an output.
+template <int DT, int D, bool EXACT>
+__global__ __launch_bounds__((Scan<DT, D, SUM>::THREADS), 2) void decay_sum_kernel(const ScanArgs a)
+{
+    using T = Scan<DT, D, SUM>;
+    constexpr int CT = T::CT, PLANES = planes<DT, EXACT>();
+    constexpr bool F16 = DT == FLARE_F16;
+    __shared__ __align__(1024) char lds[T::STAGES * T::SET];
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+    const int part = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Work work = work_of<T::GROUP>(a);
+    if (work.none) return;
+    const int h = work.bh % a.H, lead = a.reverse ? 0 : 1, len = item_length(a.lengths, work.bh / a.H, a.N);
+    const int t_begin = work.seg * a.seg_len, t_end = min(t_begin + a.seg_len, len);
+    if (t_begin >= len || (t_end == len && !a.whole)) return;      // nothing there, or nobody asks for it
+    const float g = a.log_decay[h], e2 = decay_log2(g);
+    int chunks = (t_end - t_begin + 31) / 32;
+    // What a token adds has 2^-64 of its weight left 64 halvings later, where fp32 sums no longer see it.
+    const int first = e2 < 0.f ? max(0, chunks - 1 - (int)fminf(ceilf(-2.f / e2), 0x1p24f)) : 0;
+    const Loader<T> loader(a, work.bh, len, t_end, part, lane);
+    chunks -= first;
+    const int t_first = t_begin + 32 * first;
+#pragma unroll
+    for (int i = 0; i < T::STAGES - 1; ++i)
+        if (i < chunks) loader.load(t_first + 32 * (chunks - 1 - i), lds + i * T::SET);
+
+    f32x16 acc[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) acc[ct] = splat16(0.f);
+    float wu[16];
+    const auto weights = [&](int n) {       // (a token behind the end weighs nothing)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int u = perm_index(r >> 3, hh, r & 7);
+            wu[r] = u < n ? a.m * fast_exp2(e2 * (n - lead - u)) : 0.f;
+        }
+    };
+    const int last_n = t_end - t_first - 32 * (chunks - 1);
+    weights(last_n);
+    Fade fade(g, 32);
+    float behind = 1.f;                      // the decay of what lies behind the chunk
+    int e_z = 0, stage = 0;                  // fp16: the accumulators hold the sum times down_z = 2^-e_z
+    float down_z = 1.f;
+    for (int i = 0; i < chunks; ++i) {
+        if (i + T::STAGES - 1 > chunks) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::STAGES - 2) * T::LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (i + T::STAGES - 1 < chunks)
+            loader.load(t_first + 32 * (chunks - T::STAGES - i), lds + (stage == 0 ? T::STAGES - 1 : stage - 1) * T::SET);
+        const char *const ty = lds + stage * T::SET, *const tz = ty + T::BYTES;
+        stage = stage + 1 == T::STAGES ? 0 : stage + 1;
+        const Frag<DT> zc[2] = {col_frag<DT, D, false>(tz, part, 0, lane), col_frag<DT, D, false>(tz, part, 1, lane)};
+        float weighted[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) weighted[r] = elem_of<DT>(zc[r >> 3], r & 7) * (wu[r] * (behind * down_z));
+        if constexpr (F16) {
+            const float took = fit_exponent(weighted, e_z);
+            if (took != 1.f) {
+                down_z *= took;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[ct][r] *= took;
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            Frag<DT> plane[PLANES];
+            split_planes<DT, PLANES>(weighted + 8 * ks, plane);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const Frag<DT> yc = col_frag<DT, D, true>(ty, ct, ks, lane);
+#pragma unroll
+                for (int k = 0; k < PLANES; ++k) acc[ct] = mma<DT>(yc, plane[k], acc[ct]);
+            }
+        }
+        if (i == 0 && last_n < 32) {
+            behind = fast_exp2(e2 * last_n);
+            weights(32);
+        } else {
+            behind *= fade.next();
+        }
+    }
+    float *const dst = a.slots + ((size_t)work.bh * a.segments + work.seg) * (D * D);
+    const int col = 32 * part + l32;
+    if (col < D) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = state_row(ct, r, hh);
+                if (D >= 32 || row < D) dst[(size_t)row * D + col] = F16 ? ldexpf(acc[ct][r], e_z) : acc[ct][r];
+            }
+    }
+}
+
+// The scan of a segment.  EXACT: its last state is an output (of one segment; of several it comes out of the sums).
 template <int DT, int D, int KIND, bool EXACT>
 __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::PER_SIMD)) void decay_scan_kernel(const ScanArgs a)
 {
     using T = Scan<DT, D, KIND>;
-    constexpr int STEPS = D / 16, CT = T::CT;
+    constexpr int STEPS = D / 16, CT = T::CT, PLANES = planes<DT, EXACT>();
     constexpr bool F16 = DT == FLARE_F16;
-    constexpr int PLANES = DT == FLARE_F32 ? 1 : DT == FLARE_BF16 && EXACT ? 3 : 2;
     __shared__ __align__(1024) char lds[T::STAGES * T::SET];
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave % CT, which = wave / CT;
-    // Neighbouring heads of a segment on one XCD (workgroups go round the eight): with [B][N][H][d] their rows share lines.
-    const int total = a.BH * a.segments, each = gridDim.x >> 3, work = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-    if (work >= total) return;
-    const int seg = work / a.BH, bh = work % a.BH, h = bh % a.H, job = blockIdx.y;
+    const Work work = work_of<T::GROUP>(a);
+    if (work.none) return;
+    const int seg = work.seg, bh = work.bh, h = bh % a.H;
     const Role &role = a.role[which];
-    const bool reverse = a.reverse[job] != 0;
+    const bool reverse = a.reverse != 0;
     const int lead = reverse ? 0 : 1;
     const int len = item_length(a.lengths, bh / a.H, a.N);
     const int t_begin = seg * a.seg_len, t_end = min(t_begin + a.seg_len, len);
     const size_t base = tok_base(a.ts, bh, a.H);
     const float g = a.log_decay[h], e2 = decay_log2(g);
 
-    if constexpr (KIND == SUM) {
-        if (t_begin + a.seg_len >= len) return;       // nobody reads the sum of the last segment
-    } else {
-        // rows of the padding
-        const int z0 = max(t_begin, len), z1 = min(t_begin + a.seg_len, a.N);
-        for (int q = tid % (64 * CT); q < (z1 - z0) * T::PIECES; q += 64 * CT)
-            *reinterpret_cast<u32x4 *>(static_cast<char *>(role.out) + (base + tok_off(a.ts, z0 + q / T::PIECES)) * T::ES +
-                                       q % T::PIECES * 16) = u32x4{0, 0, 0, 0};
-        if (seg != 0 && t_begin >= len) return;
-    }
+    // rows of the padding
+    const int z0 = max(t_begin, len), z1 = min(t_begin + a.seg_len, a.N);
+    for (int q = tid % (64 * CT); q < (z1 - z0) * T::PIECES; q += 64 * CT)
+        *reinterpret_cast<u32x4 *>(static_cast<char *>(role.out) + (base + tok_off(a.ts, z0 + q / T::PIECES)) * T::ES +
+                                   q % T::PIECES * 16) = u32x4{0, 0, 0, 0};
+    if (seg != 0 && t_begin >= len) return;
 
-    // ---- loads of a chunk: 16 bytes a lane, 1024 a wave, straight into LDS ----
-    const unsigned row_bytes = (unsigned)a.ts.sn * T::ES;
-    const auto offset_of = [&](int i, int valid) {      // of load i, from the chunk's first row in memory
-        const int q = (i * T::WAVES + wave) % T::TILE_LOADS * 64 + lane, r = q / T::PIECES;
-        const int c = (q % T::PIECES) ^ swizzle<T::ROW>(r), rc = min(r, valid - 1);   // behind the end: the last row again
-        return (unsigned)(reverse ? 31 - rc : rc) * row_bytes + 16 * c;
-    };
-    unsigned offset[T::LOADS];
-#pragma unroll
-    for (int i = 0; i < T::LOADS; ++i) offset[i] = offset_of(i, 32);
-    const auto load = [&](int t0, int stage) {
-        const int n0 = reverse ? len - 32 - t0 : t0, valid = t_end - t0;
-        const long long at = ((long long)base + (long long)n0 * (long long)a.ts.sn) * T::ES;
-#pragma unroll
-        for (int i = 0; i < T::LOADS; ++i) {
-            const int k = i * T::WAVES + wave;
-            const char *src = static_cast<const char *>(a.in[job][k / T::TILE_LOADS]) + at;
-            const unsigned off = valid >= 32 ? offset[i] : offset_of(i, valid);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + off),
-                                             (__attribute__((address_space(3))) void *)(lds + stage * T::SET + k * 1024), 16, 0, 0);
-        }
-    };
+    const Loader<T> loader(a, bh, len, t_end, wave, lane);
     const int chunks = t_begin < t_end ? (t_end - t_begin + 31) / 32 : 0;
 #pragma unroll
     for (int i = 0; i < T::STAGES - 1; ++i)
-        if (i < chunks) load(t_begin + 32 * i, i);
+        if (i < chunks) loader.load(t_begin + 32 * i, lds + i * T::SET);
 
     // the state before the segment: column 32 part + l32
     f32x16 acc[CT];
     const int col = 32 * part + l32;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc[ct] = splat16(0.f);
-    const size_t slot = (((size_t)job * a.BH + bh) * a.segments + seg) * (D * D);
-    if constexpr (KIND != SUM) {
-        const float *s = a.segments > 1 ? a.slots + slot : role.first ? role.first + (size_t)bh * (D * D) : nullptr;
+    {
+        const float *s = a.slots ? a.slots + ((size_t)bh * a.segments + seg) * (D * D) : role.first ? role.first + (size_t)bh * (D * D) : nullptr;
         if (s && col < D) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
@@ -286,87 +448,106 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
     }
 
     // weights, as far as they are the same in every chunk
-    float wp[16], wi = 0.f, wu[16];
-    if constexpr (KIND != SUM) {
+    float wp[16], wu[16];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int gap = l32 - perm_index(r >> 3, hh, r & 7);
-            wp[r] = gap >= 0 ? a.p * fast_exp2(e2 * gap) : 0.f;
-        }
-        wi = a.w * fast_exp2(e2 * (l32 + lead));
+    for (int r = 0; r < 16; ++r) {
+        const int gap = l32 - perm_index(r >> 3, hh, r & 7);
+        wp[r] = gap >= 0 ? a.p * fast_exp2(e2 * gap) : 0.f;
     }
+    const float wi = a.w * fast_exp2(e2 * (l32 + lead));
     const auto update_weights = [&](int n) {       // (a token behind the end weighs nothing)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int u = perm_index(r >> 3, hh, r & 7);
-            wu[r] = u < n ? a.m[job] * fast_exp2(e2 * (n - lead - u)) : 0.f;
+            wu[r] = u < n ? a.m * fast_exp2(e2 * (n - lead - u)) : 0.f;
         }
     };
     update_weights(32);
     Fade fade(g, 32);
-    int e_state = 0, e_p = 0, e_z = 0;    // fp16: of the state as an operand, of P, of the weighted z (the accumulators hold C 2^-e_z)
+    // The accumulators hold C / (f 2^e_z).  With slow decays f takes up the decay of the chunks, and is multiplied in where it has
+    // become small; otherwise (a chunk leaves less than 2^-16) the accumulators themselves are multiplied in each chunk.
+    float f = 1.f;
+    // fp16: exponents of the weighted z, of P (in wp too) and of the state as an operand
+    int e_z = 0, e_p = 0, e_state = 0;
+    float down_z = 1.f, down_state = 1.f;
 
     // tiles of this wave's role
-    constexpr int X = KIND == FORWARD ? 0 : -1, Y = KIND == SUM ? 0 : KIND == FORWARD ? 1 : -1, Z = KIND == SUM ? 1 : KIND == FORWARD ? 2 : -1;
-    const int x_at = (KIND == DKDV ? (which ? 1 : 2) : X) * T::BYTES, y_at = (KIND == DKDV ? (which ? 0 : 3) : Y) * T::BYTES,
-              z_at = (KIND == DKDV ? (which ? 3 : 0) : Z) * T::BYTES;
+    const int x_at = (KIND == FORWARD ? 0 : which ? 1 : 2) * T::BYTES, y_at = (KIND == FORWARD ? 1 : which ? 0 : 3) * T::BYTES,
+              z_at = (KIND == FORWARD ? 2 : which ? 3 : 0) * T::BYTES;
 
-    int stage = 0;
-    for (int i = 0; i < chunks; ++i) {
-        const int t0 = t_begin + 32 * i;
-        // This wave's part of chunk i is there when no more is on its way than what was asked for behind it: the loads of
-        // STAGES - 2 chunks, and the stores of the chunks since (full ones; the barrier makes it everyone's part).  Its own reads
-        // of chunk i - 1 have returned.
-        if (i + T::STAGES - 1 > chunks) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        else if (i < T::STAGES - 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::STAGES - 2) * T::LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::STAGES - 2) * T::LOADS + (T::STAGES - 1) * T::STORES) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        // (everyone is done with chunk i - 1, whose place this takes)
-        if (i + T::STAGES - 1 < chunks) load(t0 + 32 * (T::STAGES - 1), stage == 0 ? T::STAGES - 1 : stage - 1);
-        const char *const set = lds + stage * T::SET;
+    // One chunk.  PLAIN: of 32 tokens, and slow decays.  The weighted z goes in planes: what the state sums is then good to 2^-22
+    // (fp16) or 2^-24 (bf16) of a term; a state that is no output only meets x rounded to 16 bits, and 2^-16 will do with bf16.
+    const auto chunk = [&](auto plain_tag, int t0, const char *set) {
+        constexpr bool PLAIN = decltype(plain_tag)::value;
         const char *const tx = set + x_at, *const ty = set + y_at, *const tz = set + z_at;
-        const int valid = t_end - t0;
+        __builtin_amdgcn_s_setprio(1);       // (the waves of a SIMD then are less often in the same part)
         float faded = fade.next();
-        if (valid < 32) {
-            update_weights(valid);
-            faded = fast_exp2(e2 * valid);
+        if (!PLAIN && t0 + 32 > t_end) {
+            update_weights(t_end - t0);
+            faded = fast_exp2(e2 * (t_end - t0));
         }
 
         const Frag<DT> zc[2] = {col_frag<DT, D, false>(tz, part, 0, lane), col_frag<DT, D, false>(tz, part, 1, lane)};
-        if constexpr (KIND != SUM) {
-            float scale_state = 1.f;
+        {
+            Frag<DT> state[STEPS];
             if constexpr (F16) {
-                float largest = 0.f;
+                for (;;) {
+                    // (one overflow, and the sum of squares is infinite)
+                    float squares = 0.f;
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
+                    for (int s = 0; s < STEPS; ++s) {
+                        float c8[8];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(acc[ct][r]));
-                fit_exponent(e_state, largest);
-                scale_state = ldexpf(1.f, -e_state);
+                        for (int e = 0; e < 8; ++e) c8[e] = acc[s >> 1][8 * (s & 1) + e] * down_state;
+                        state[s] = pack8<DT>(c8);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const f16x2 two = __builtin_bit_cast(f16x2, state[s].w[e]);
+                            squares = __builtin_amdgcn_fdot2(two, two, squares, false);
+                        }
+                    }
+                    int step = 0;
+                    if (__any(squares > 0x1p30f)) {
+                        step = e_state < 96 ? kExponentStep : 0;
+                    } else if (!__any(squares >= 16.f)) {       // (all of them may have vanished: by the fp32 values)
+                        float largest = 0.f;
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(acc[ct][r] * down_state));
+                        step = exponent_step(largest, e_state);
+                    }
+                    if (step == 0) break;
+                    e_state += step;
+                    down_state = ldexpf(1.f, -e_state);
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    float c8[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) c8[e] = acc[s >> 1][8 * (s & 1) + e];
+                    state[s] = pack8<DT>(c8);
+                }
             }
             f32x16 p = splat16(0.f), o = splat16(0.f);
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 const Frag<DT> xf = row_frag<DT, D>(tx, l32, s, hh), yf = row_frag<DT, D>(ty, l32, s, hh);
                 p = mma<DT>(yf, xf, p);
-                float c8[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) c8[e] = F16 ? acc[s >> 1][8 * (s & 1) + e] * scale_state : acc[s >> 1][8 * (s & 1) + e];
-                o = mma<DT>(pack8<DT>(c8), xf, o);
+                o = mma<DT>(state[s], xf, o);
             }
+            float p16[16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] *= wp[r];
-            float scale_o = wi, scale_out = 1.f;
+            for (int r = 0; r < 16; ++r) p16[r] = p[r] * wp[r];
+            float scale_o = wi * f, scale_out = 1.f;
             if constexpr (F16) {
-                float largest = 0.f;
+                const float took = fit_exponent(p16, e_p);
+                if (took != 1.f) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(p[r]));
-                fit_exponent(e_p, largest);
-                const float down = ldexpf(1.f, -e_p);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] *= down;
-                scale_o = ldexpf(wi, e_state + e_z - e_p);
+                    for (int r = 0; r < 16; ++r) wp[r] *= took;
+                }
+                scale_o = ldexpf(scale_o, e_state + e_z - e_p);
                 scale_out = ldexpf(1.f, e_p);
             }
 #pragma unroll
@@ -375,70 +556,66 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
             for (int ks = 0; ks < 2; ++ks) {
                 float p8[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p8[e] = p[8 * ks + e];
+                for (int e = 0; e < 8; ++e) p8[e] = p16[8 * ks + e];
                 o = mma<DT>(zc[ks], pack8<DT>(p8), o);
             }
             const int t = t0 + l32;
-            if (t < t_end) {
-                char *const row = static_cast<char *>(role.out) +
-                                  (base + tok_off(a.ts, reverse ? len - 1 - t : t) + 32 * part) * T::ES;
-                if constexpr (F16) {
+            char *const row = static_cast<char *>(role.out) +
+                              (base + tok_off(a.ts, reverse ? len - 1 - t : t) + 32 * part) * T::ES;
+            if constexpr (F16) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) o[r] *= scale_out;
-                }
-                if constexpr (DT == FLARE_F32) {
+                for (int r = 0; r < 16; ++r) o[r] *= scale_out;
+            }
+            if constexpr (DT == FLARE_F32) {
 #pragma unroll
-                    for (int q = 0; q < (D < 32 ? 2 : 4); ++q)
+                for (int q = 0; q < (D < 32 ? 2 : 4); ++q)
+                    if (PLAIN || t < t_end)
                         *reinterpret_cast<float4 *>(row + (8 * q + 4 * hh) * 4) =
                             make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-                } else {
-                    // register group q holds columns 8 q + 4 hh + 0..3: the halves of the wave trade groups, for 16 bytes a lane
+            } else {
+                // register group q holds columns 8 q + 4 hh + 0..3: the halves of the wave trade groups, for 16 bytes a lane
 #pragma unroll
-                    for (int q = 0; q < (D < 32 ? 1 : 2); ++q) {
-                        u32x4 w;
+                for (int q = 0; q < (D < 32 ? 1 : 2); ++q) {
+                    u32x4 w;
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const auto both = __builtin_amdgcn_permlane32_swap(pack_elems<F16>(o[8 * q + 2 * k], o[8 * q + 2 * k + 1]),
-                                                                               pack_elems<F16>(o[8 * q + 4 + 2 * k], o[8 * q + 5 + 2 * k]),
-                                                                               false, false);
-                            w[k] = both[0];
-                            w[2 + k] = both[1];
-                        }
-                        *reinterpret_cast<u32x4 *>(row + (16 * q + 8 * hh) * 2) = w;
+                    for (int k = 0; k < 2; ++k) {
+                        const auto both = __builtin_amdgcn_permlane32_swap(pack_elems<F16>(o[8 * q + 2 * k], o[8 * q + 2 * k + 1]),
+                                                                           pack_elems<F16>(o[8 * q + 4 + 2 * k], o[8 * q + 5 + 2 * k]),
+                                                                           false, false);
+                        w[k] = both[0];
+                        w[2 + k] = both[1];
                     }
+                    if (PLAIN || t < t_end) *reinterpret_cast<u32x4 *>(row + (16 * q + 8 * hh) * 2) = w;
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
+        sched_fence();
+        if constexpr (PLAIN) f *= faded;
         float weighted[16];
+        const float lift = PLAIN ? down_z / f : down_z;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) weighted[r] = elem_of<DT>(zc[r >> 3], r & 7) * wu[r];
+        for (int r = 0; r < 16; ++r) weighted[r] = elem_of<DT>(zc[r >> 3], r & 7) * (PLAIN || F16 ? wu[r] * lift : wu[r]);
         if constexpr (F16) {
-            float largest = 0.f;
+            const float took = fit_exponent(weighted, e_z);
+            if (took != 1.f) {
+                down_z *= took;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(weighted[r]));
-            const int before = e_z;
-            fit_exponent(e_z, largest);
-            faded = ldexpf(faded, before - e_z);
-            const float down = ldexpf(1.f, -e_z);
+                for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) weighted[r] *= down;
+                    for (int r = 0; r < 16; ++r) acc[ct][r] *= took;
+            }
+        }
+        if constexpr (!PLAIN) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[ct][r] *= faded;
         }
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[ct][r] *= faded;
-#pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            float left[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) left[e] = weighted[8 * ks + e];
             Frag<DT> plane[PLANES];
-#pragma unroll
-            for (int k = 0; k < PLANES; ++k) {
-                plane[k] = pack8<DT>(left);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) left[e] -= elem_of<DT>(plane[k], e);
-            }
+            split_planes<DT, PLANES>(weighted + 8 * ks, plane);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 const Frag<DT> yc = col_frag<DT, D, true>(ty, ct, ks, lane);
@@ -446,12 +623,46 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
                 for (int k = 0; k < PLANES; ++k) acc[ct] = mma<DT>(yc, plane[k], acc[ct]);
             }
         }
+    };
+    int i = 0, stage = 0;
+    const auto next_chunk = [&]() {
+        // This wave's part of chunk i is there when no more is on its way than what was asked for behind it: the loads of
+        // STAGES - 2 chunks, and the stores of the chunks since (full ones; the barrier makes it everyone's part).  Its own
+        // reads of chunk i - 1 have returned.
+        if (i + T::STAGES - 1 > chunks) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        else if (i < T::STAGES - 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::STAGES - 2) * T::LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((T::STAGES - 2) * T::LOADS + (T::STAGES - 1) * T::STORES) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // (everyone is done with chunk i - 1, whose place this takes)
+        if (i + T::STAGES - 1 < chunks)
+            loader.load(t_begin + 32 * (i + T::STAGES - 1), lds + (stage == 0 ? T::STAGES - 1 : stage - 1) * T::SET);
+        const char *const set = lds + stage * T::SET;
         stage = stage + 1 == T::STAGES ? 0 : stage + 1;
+        return set;
+    };
+    const auto take_up = [&]() {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[ct][r] *= f;
+        f = 1.f;
+    };
+    if (fade.down >= kSlow) {
+        const int full = t_begin < t_end ? (t_end - t_begin) / 32 : 0;
+        for (; i < full; ++i) {
+            const char *const set = next_chunk();
+            if (f < kSlow) take_up();
+            chunk(PlainTag<true>{}, t_begin + 32 * i, set);
+        }
+        take_up();
+    }
+    for (; i < chunks; ++i) {
+        const char *const set = next_chunk();
+        chunk(PlainTag<false>{}, t_begin + 32 * i, set);
     }
 
-    float *dst = nullptr;
-    if constexpr (KIND == SUM) dst = a.slots + slot;
-    else if (role.last && t_begin + a.seg_len >= len) dst = role.last + (size_t)bh * (D * D);
+    float *const dst = role.last ? role.last + (size_t)bh * (D * D) : nullptr;
     if (dst && col < D) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
@@ -465,8 +676,8 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
 
 // Segments' sums -> the state before each segment, in place: thread = four neighbouring entries of a state.
 struct CarryArgs {
-    const float *first[2];   // state before the first token of either job, or NULL
-    int turned[2];
+    const float *first;      // state before the first token, or NULL
+    float *last;             // state behind the last one, or NULL
     const float *log_decay;
     const int *lengths;
     float *slots;
@@ -475,31 +686,36 @@ struct CarryArgs {
 __global__ __launch_bounds__(256) void decay_carry_kernel(const CarryArgs a)
 {
     const int d = a.d, dd = d * d, tiles = (dd / 4 + 255) / 256;
-    const int i = 4 * (blockIdx.x % tiles * 256 + threadIdx.x), jbh = blockIdx.x / tiles;
+    const int i = 4 * (blockIdx.x % tiles * 256 + threadIdx.x), bh = blockIdx.x / tiles;
     if (i >= dd) return;
-    const int bh = jbh % a.BH, jb = jbh / a.BH;
     const int len = item_length(a.lengths, bh / a.H, a.N);
-    const int used = (len + a.seg_len - 1) / a.seg_len;
-    Fade fade(a.log_decay[bh % a.H], a.seg_len);
+    const int used = (len + a.seg_len - 1) / a.seg_len, sums = a.last ? used : used - 1;
+    const float g = a.log_decay[bh % a.H];
+    // The sums are asked for AHEAD segments before they are added (the slots are written over behind).
+    constexpr int AHEAD = 8;
+    float *const slot = a.slots + (size_t)bh * a.segments * dd + i;
+    float4 u[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+        if (k < sums) u[k] = *reinterpret_cast<const float4 *>(slot + (size_t)k * dd);
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (a.first[jb]) {
-        const float *f = a.first[jb] + (size_t)bh * dd;
-        if (a.turned[jb]) {
-            const int row = i / d, col = i % d;
-            s = make_float4(f[(size_t)col * d + row], f[(size_t)(col + 1) * d + row], f[(size_t)(col + 2) * d + row],
-                            f[(size_t)(col + 3) * d + row]);
-        } else {
-            s = *reinterpret_cast<const float4 *>(f + i);
+    if (a.first) s = *reinterpret_cast<const float4 *>(a.first + (size_t)bh * dd + i);
+    Fade fade(g, a.seg_len);
+    for (int g0 = 0; g0 < max(used, 1); g0 += AHEAD) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int at = g0 + k;
+            if (at >= max(used, 1)) break;
+            const float4 v = u[k];
+            if (at + AHEAD < sums) u[k] = *reinterpret_cast<const float4 *>(slot + (size_t)(at + AHEAD) * dd);
+            *reinterpret_cast<float4 *>(slot + (size_t)at * dd) = s;
+            if (at < sums) {
+                const float f = at + 1 < used ? fade.next() : fast_exp2(decay_log2(g) * (float)(len - at * a.seg_len));
+                s = make_float4(fmaf(s.x, f, v.x), fmaf(s.y, f, v.y), fmaf(s.z, f, v.z), fmaf(s.w, f, v.w));
+            }
         }
     }
-    float *slot = a.slots + (size_t)jbh * a.segments * dd + i;
-    for (int g = 0; g < max(used, 1); ++g, slot += dd) {
-        float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (g + 1 < used) u = *reinterpret_cast<const float4 *>(slot);
-        *reinterpret_cast<float4 *>(slot) = s;
-        const float f = fade.next();
-        s = make_float4(fmaf(s.x, f, u.x), fmaf(s.y, f, u.y), fmaf(s.z, f, u.z), fmaf(s.w, f, u.w));
-    }
+    if (a.last) *reinterpret_cast<float4 *>(a.last + (size_t)bh * dd + i) = s;
 }
 
 // ---- one token -------------------------------------------------------------------------------------------------
@@ -575,9 +791,16 @@ TokStride decay_stride(const flare_decay_shape &s)
 struct DecayPlan { int segments, seg_len; };
 DecayPlan decay_plan(const flare_decay_shape &s, bool backward)
 {
+    // As many segments as keep the scan's waves resident together (two on a SIMD; fp32 from d = 64 on: one).  The backward's
+    // workgroups have waves in two roles: from d = 64 on half as many segments fill the chip.
     const long long waves = (s.d < 32 ? 1 : s.d / 32) * (long long)s.B * s.H;
-    long long want = (2048 + waves - 1) / waves;
-    const long long most = (s.N + 255) / 256;
+    const long long room = s.d >= 64 && (backward || s.dtype == FLARE_F32) ? 1024 : 2048;
+    long long want = room / waves;
+    // Sums and carry cost two launches, about 13 us: as much as 12 chunks one after the other (fp32: 4).  And each segment costs the
+    // carry 0.2 us, each chunk of a segment both passes 1.6 us: together least at sqrt(5 N) tokens a segment.  (8 heads of
+    // 1000 tokens, d = 64: 36 us in one, 24 us in segments of 256, 18 us of 128.)
+    const long long least = (long long)(sqrt(5.0 * s.N) / 32.0 + 0.5) * 32;
+    const long long most = s.N <= (s.dtype == FLARE_F32 ? 128 : 384) ? 1 : (s.N + least - 1) / least;
     if (want > most) want = most;
     if (want < 1) want = 1;
     const long long len = ((s.N + want - 1) / want + 31) / 32 * 32;
@@ -586,7 +809,7 @@ DecayPlan decay_plan(const flare_decay_shape &s, bool backward)
 size_t slot_bytes(const flare_decay_shape &s, bool backward)
 {
     const DecayPlan p = decay_plan(s, backward);
-    return p.segments > 1 ? (size_t)(backward ? 2 : 1) * s.B * s.H * p.segments * s.d * s.d * 4 : 0;
+    return p.segments > 1 ? (size_t)s.B * s.H * p.segments * s.d * s.d * 4 : 0;
 }
 
 // What the host knows of a call, whatever its type and d.
@@ -595,19 +818,22 @@ struct DecayCall {
     const void *q, *k, *v, *d_o;
     const float *log_decay;
     const int *lengths;
-    const float *state_in, *dstate_out;
+    const float *state_in, *dstate_out, *marks_in;
     void *o, *dq, *dk, *dv;
     float *state_out, *dstate_in;
     float scale;
-    float *slots;
+    float *slots;        // of the forward: its marks, if they are asked for
     hipStream_t stream;
 };
-ScanArgs scan_args(const DecayCall &c, const DecayPlan &p)
+ScanArgs scan_args(const DecayCall &c, const DecayPlan &p, const void *in0, const void *in1, const void *in2, const void *in3)
 {
     ScanArgs a{};
+    a.in[0] = in0;
+    a.in[1] = in1;
+    a.in[2] = in2;
+    a.in[3] = in3;
     a.log_decay = c.log_decay;
     a.lengths = c.lengths;
-    a.slots = c.slots;
     a.ts = decay_stride(*c.s);
     a.H = c.s->H;
     a.N = c.s->N;
@@ -616,33 +842,52 @@ ScanArgs scan_args(const DecayCall &c, const DecayPlan &p)
     a.seg_len = p.seg_len;
     return a;
 }
-template <int DT, int D, int KIND>
-void launch_scan(const ScanArgs &a, int jobs, bool exact, int kid, hipStream_t stream)
+template <typename T>
+unsigned scan_blocks(const ScanArgs &a)
 {
-    const dim3 grid((unsigned)((a.BH * (long long)a.segments + 7) / 8 * 8), jobs);
-    LaunchTimer timer(kid, stream);
-    if (exact && DT == FLARE_BF16)       // (the other types make no difference)
-        decay_scan_kernel<DT, D, KIND, DT == FLARE_BF16><<<grid, Scan<DT, D, KIND>::THREADS, 0, stream>>>(a);
-    else
-        decay_scan_kernel<DT, D, KIND, false><<<grid, Scan<DT, D, KIND>::THREADS, 0, stream>>>(a);
+    const long long round = 8 * T::GROUP;
+    return (unsigned)((a.BH * (long long)a.segments + round - 1) / round * round);
 }
-void launch_carry(const DecayCall &c, const DecayPlan &p, int jobs, const float *first0, int turned0, const float *first1)
+template <int DT, int D, int KIND>
+void launch_scan(const ScanArgs &a, bool exact, int kid, hipStream_t stream)
 {
-    CarryArgs a{};
-    a.first[0] = first0;
-    a.first[1] = first1;
-    a.turned[0] = turned0;
-    a.log_decay = c.log_decay;
-    a.lengths = c.lengths;
-    a.slots = c.slots;
-    a.H = c.s->H;
-    a.N = c.s->N;
-    a.BH = c.s->B * c.s->H;
-    a.segments = p.segments;
-    a.seg_len = p.seg_len;
-    a.d = c.s->d;
+    using T = Scan<DT, D, KIND>;
+    LaunchTimer timer(kid, stream);
+    if (exact && DT == FLARE_BF16)       // (to the other types it makes no difference)
+        decay_scan_kernel<DT, D, KIND, DT == FLARE_BF16><<<scan_blocks<T>(a), T::THREADS, 0, stream>>>(a);
+    else
+        decay_scan_kernel<DT, D, KIND, false><<<scan_blocks<T>(a), T::THREADS, 0, stream>>>(a);
+}
+// The states before the segments of the scan (x), y, z, into slots, and the state behind the last (or NULL).
+template <int DT, int D>
+void launch_states(const DecayCall &c, const DecayPlan &p, const void *y, const void *z, float m, bool reverse, const float *first,
+                   float *last, float *slots)
+{
+    using T = Scan<DT, D, SUM>;
+    ScanArgs a = scan_args(c, p, y, z, nullptr, nullptr);
+    a.slots = slots;
+    a.m = m;
+    a.reverse = reverse;
+    a.whole = last != nullptr;
+    {
+        LaunchTimer timer(KID_DECAY_SUM, c.stream);
+        if (last && DT == FLARE_BF16) decay_sum_kernel<DT, D, DT == FLARE_BF16><<<scan_blocks<T>(a), T::THREADS, 0, c.stream>>>(a);
+        else decay_sum_kernel<DT, D, false><<<scan_blocks<T>(a), T::THREADS, 0, c.stream>>>(a);
+    }
+    CarryArgs b{};
+    b.first = first;
+    b.last = last;
+    b.log_decay = c.log_decay;
+    b.lengths = c.lengths;
+    b.slots = slots;
+    b.H = a.H;
+    b.N = a.N;
+    b.BH = a.BH;
+    b.segments = p.segments;
+    b.seg_len = p.seg_len;
+    b.d = D;
     LaunchTimer timer(KID_DECAY_CARRY, c.stream);
-    decay_carry_kernel<<<(a.d * a.d / 4 + 255) / 256 * a.BH * jobs, 256, 0, c.stream>>>(a);
+    decay_carry_kernel<<<(D * D / 4 + 255) / 256 * a.BH, 256, 0, c.stream>>>(b);
 }
 
 struct ForwardPass {
@@ -650,23 +895,14 @@ struct ForwardPass {
     static int run(const DecayCall &c)
     {
         const DecayPlan p = decay_plan(*c.s, false);
-        const bool exact = c.state_out != nullptr;
-        if (p.segments > 1) {
-            ScanArgs a = scan_args(c, p);
-            a.in[0][0] = c.k;
-            a.in[0][1] = c.v;
-            a.m[0] = 1.f;
-            launch_scan<DT, D, SUM>(a, 1, exact, KID_DECAY_SUM, c.stream);
-            launch_carry(c, p, 1, c.state_in, 0, nullptr);
-        }
-        ScanArgs a = scan_args(c, p);
-        a.in[0][0] = c.q;
-        a.in[0][1] = c.k;
-        a.in[0][2] = c.v;
-        a.role[0] = Role{c.o, c.state_in, c.state_out, 0};
+        const bool split = p.segments > 1;
+        if (split) launch_states<DT, D>(c, p, c.k, c.v, 1.f, false, c.state_in, c.state_out, c.slots);
+        ScanArgs a = scan_args(c, p, c.q, c.k, c.v, nullptr);
+        a.slots = split ? c.slots : nullptr;
+        a.role[0] = Role{c.o, c.state_in, split ? nullptr : c.state_out, 0};
         a.p = a.w = c.scale;
-        a.m[0] = 1.f;
-        launch_scan<DT, D, FORWARD>(a, 1, exact, KID_DECAY_FORWARD, c.stream);
+        a.m = 1.f;
+        launch_scan<DT, D, FORWARD>(a, a.role[0].last != nullptr, KID_DECAY_FORWARD, c.stream);
         return check_launch();
     }
 };
@@ -674,43 +910,33 @@ struct BackwardPass {
     template <int DT, int D>
     static int run(const DecayCall &c)
     {
-        const DecayPlan p = decay_plan(*c.s, true);
-        const bool exact = c.dstate_in != nullptr;
-        if (p.segments > 1) {
-            // job 0: the transposed S (rows by v), forwards; job 1: its gradient (rows by q), backwards
-            ScanArgs a = scan_args(c, p);
-            a.in[0][0] = c.v;
-            a.in[0][1] = c.k;
-            a.in[1][0] = c.q;
-            a.in[1][1] = c.d_o;
-            a.m[0] = 1.f;
-            a.m[1] = c.scale;
-            a.reverse[1] = 1;
-            launch_scan<DT, D, SUM>(a, 2, exact, KID_DECAY_SUM, c.stream);
-            launch_carry(c, p, 2, c.state_in, 1, c.dstate_out);
+        // dQ: cut as the forward is, from its states S (transposed: rows by v)
+        DecayPlan p = decay_plan(*c.s, false);
+        bool split = p.segments > 1;
+        const float *marks = c.marks_in;
+        if (split && !marks) {
+            launch_states<DT, D>(c, p, c.k, c.v, 1.f, false, c.state_in, nullptr, c.slots);
+            marks = c.slots;
         }
-        const bool slots = p.segments > 1;
-        ScanArgs a = scan_args(c, p);
-        a.in[0][0] = c.d_o;
-        a.in[0][1] = c.v;
-        a.in[0][2] = c.k;
-        a.role[0] = Role{c.dq, c.state_in, nullptr, slots ? 0 : 1};
+        ScanArgs a = scan_args(c, p, c.d_o, c.v, c.k, nullptr);
+        a.slots = split ? const_cast<float *>(marks) : nullptr;
+        a.role[0] = Role{c.dq, c.state_in, nullptr, 1};
         a.p = a.w = c.scale;
-        a.m[0] = 1.f;
-        launch_scan<DT, D, FORWARD>(a, 1, false, KID_DECAY_DQ, c.stream);
-        a = scan_args(c, p);
-        a.in[0][0] = c.q;
-        a.in[0][1] = c.k;
-        a.in[0][2] = c.v;
-        a.in[0][3] = c.d_o;
-        a.role[0] = Role{c.dk, c.dstate_out, nullptr, 1};            // x = v, y = dO, z = q
-        a.role[1] = Role{c.dv, c.dstate_out, c.dstate_in, 0};        // x = k, y = q, z = dO
+        a.m = 1.f;
+        launch_scan<DT, D, FORWARD>(a, false, KID_DECAY_DQ, c.stream);
+        // dK and dV: from the gradient of S (rows by q), time running backwards
+        p = decay_plan(*c.s, true);
+        split = p.segments > 1;
+        if (split) launch_states<DT, D>(c, p, c.q, c.d_o, c.scale, true, c.dstate_out, c.dstate_in, c.slots);
+        a = scan_args(c, p, c.q, c.k, c.v, c.d_o);
+        a.slots = split ? c.slots : nullptr;
+        a.role[0] = Role{c.dk, c.dstate_out, nullptr, 1};                                  // x = v, y = dO, z = q
+        a.role[1] = Role{c.dv, c.dstate_out, split ? nullptr : c.dstate_in, 0};            // x = k, y = q, z = dO
         a.p = c.scale;
         a.w = 1.f;
-        a.m[0] = c.scale;
-        a.reverse[0] = 1;
-        if (slots) a.slots += (size_t)a.BH * p.segments * D * D;
-        launch_scan<DT, D, DKDV>(a, 1, exact, KID_DECAY_DKDV, c.stream);
+        a.m = c.scale;
+        a.reverse = 1;
+        launch_scan<DT, D, DKDV>(a, a.role[1].last != nullptr, KID_DECAY_DKDV, c.stream);
         return check_launch();
     }
 };
@@ -764,11 +990,16 @@ int run_step_d(const flare_decay_shape &s, const void *q, const void *k, const v
 
 }  // namespace
 
-size_t decay_fwd_bytes(const flare_decay_shape &s) { return slot_bytes(s, false); }
-size_t decay_bwd_bytes(const flare_decay_shape &s) { return slot_bytes(s, true); }
+size_t decay_marks_bytes(const flare_decay_shape &s) { return slot_bytes(s, false); }
+size_t decay_fwd_bytes(const flare_decay_shape &s, bool marks) { return marks ? 0 : slot_bytes(s, false); }
+size_t decay_bwd_bytes(const flare_decay_shape &s, bool marks)
+{
+    const size_t states = marks ? 0 : slot_bytes(s, false), gradients = slot_bytes(s, true);   // one after the other
+    return states > gradients ? states : gradients;
+}
 
 int decay_forward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
-                  const int *lengths, const float *state_in, void *o, float *state_out, float scale, void *ws,
+                  const int *lengths, const float *state_in, void *o, float *state_out, float *marks, float scale, void *ws,
                   hipStream_t stream)
 {
     DecayCall c{};
@@ -782,14 +1013,14 @@ int decay_forward(const flare_decay_shape &s, const void *q, const void *k, cons
     c.o = o;
     c.state_out = state_out;
     c.scale = scale;
-    c.slots = static_cast<float *>(ws);
+    c.slots = marks ? marks : static_cast<float *>(ws);
     c.stream = stream;
     return run_pass<ForwardPass>(c);
 }
 
 int decay_backward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
-                   const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq, void *dk,
-                   void *dv, float *dstate_in, float scale, void *ws, hipStream_t stream)
+                   const int *lengths, const float *state_in, const float *marks, const void *d_o, const float *dstate_out,
+                   void *dq, void *dk, void *dv, float *dstate_in, float scale, void *ws, hipStream_t stream)
 {
     DecayCall c{};
     c.s = &s;
@@ -800,6 +1031,7 @@ int decay_backward(const flare_decay_shape &s, const void *q, const void *k, con
     c.log_decay = log_decay;
     c.lengths = lengths;
     c.state_in = state_in;
+    c.marks_in = marks;
     c.dstate_out = dstate_out;
     c.dq = dq;
     c.dk = dk;

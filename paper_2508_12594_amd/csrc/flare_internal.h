@@ -196,15 +196,16 @@ size_t spectral_bytes(const flare_shape &s);
 int spectral_run(const flare_shape &s, const void *q, const void *k, const float *lse_enc, const float *lse_dec,
                  float scale, int first, float *evals, float *zvec, float *gram, void *ws, hipStream_t stream);
 
-// ---- decay mixer (flare_decay.hip); state_in, lengths, state_out, dstate_* and active may be NULL ----------
-size_t decay_fwd_bytes(const flare_decay_shape &s);
-size_t decay_bwd_bytes(const flare_decay_shape &s);
+// ---- decay mixer (flare_decay.hip); state_in, lengths, marks, state_out, dstate_* and active may be NULL ----------
+size_t decay_marks_bytes(const flare_decay_shape &s);
+size_t decay_fwd_bytes(const flare_decay_shape &s, bool marks);    // marks: are they written (read)?
+size_t decay_bwd_bytes(const flare_decay_shape &s, bool marks);
 int decay_forward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
-                  const int *lengths, const float *state_in, void *o, float *state_out, float scale, void *ws,
+                  const int *lengths, const float *state_in, void *o, float *state_out, float *marks, float scale, void *ws,
                   hipStream_t stream);
 int decay_backward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
-                   const int *lengths, const float *state_in, const void *d_o, const float *dstate_out, void *dq, void *dk,
-                   void *dv, float *dstate_in, float scale, void *ws, hipStream_t stream);
+                   const int *lengths, const float *state_in, const float *marks, const void *d_o, const float *dstate_out,
+                   void *dq, void *dk, void *dv, float *dstate_in, float scale, void *ws, hipStream_t stream);
 int decay_step(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay, const int *active,
                const float *state_in, float *state_out, void *o, float scale, hipStream_t stream);
 

@@ -552,12 +552,21 @@ flare_decay_shape decay_shape_of(const Tensor &q, int layout)
 }
 const float *cf32(const void *p) { return static_cast<const float *>(p); }
 const int *ci32(const void *p) { return static_cast<const int *>(p); }
-size_t decay_bytes(const flare_decay_shape &s, bool backward)
+struct DecayBytes { size_t forward = 0, backward = 0, marks = 0; };
+DecayBytes decay_bytes(const flare_decay_shape &s)
 {
-    size_t n = 0;
-    check(backward ? lib.decay_workspace_bytes(&s, nullptr, &n) : lib.decay_workspace_bytes(&s, &n, nullptr),
-          "flare_decay_workspace_bytes");
+    DecayBytes n;
+    check(lib.decay_workspace_bytes(&s, &n.forward, &n.backward, &n.marks), "flare_decay_workspace_bytes");
     return n;
+}
+// marks that the caller brought: fp32, of any shape
+void *marks_ptr(const OptTensor &t, size_t bytes)
+{
+    if (!t) return nullptr;
+    void *const p = dev(*t, "marks");
+    if (t->scalar_type() != at::kFloat || (size_t)t->numel() * 4 < bytes)
+        throw Error("marks must be float32 and hold " + std::to_string(bytes) + " bytes");
+    return p;
 }
 // Needs none: no block is asked of the allocator.
 Workspace decay_workspace(size_t need, const OptTensor &given, const Tensor &like, const Target &to)
@@ -568,26 +577,26 @@ Workspace decay_workspace(size_t need, const OptTensor &given, const Tensor &lik
 
 std::tuple<Tensor, OptTensor> decay_forward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay, double scale,
                                             const OptTensor &lengths, const OptTensor &state, const OptTensor &o_in,
-                                            const OptTensor &state_out_in, bool want_state, const OptTensor &ws_in,
-                                            const py::object &stream, int layout)
+                                            const OptTensor &state_out_in, bool want_state, const OptTensor &marks,
+                                            const OptTensor &ws_in, const py::object &stream, int layout)
 {
     const OptTensor ok = k, ov = v, og = log_decay;
-    const c10::DeviceGuard guard(one_device(q, "q", {&ok, &ov, &og, &lengths, &state, &o_in, &state_out_in, &ws_in}));
+    const c10::DeviceGuard guard(one_device(q, "q", {&ok, &ov, &og, &lengths, &state, &o_in, &state_out_in, &marks, &ws_in}));
     const flare_decay_shape s = decay_shape_of(q, layout);
     const DecayDims dim(s);
     const Target to = target(stream, !ws_in);
     const py::gil_scoped_release no_gil;
     const at::ScalarType dt = q.scalar_type();
-    const size_t need = decay_bytes(s, false);
+    const DecayBytes need = decay_bytes(s);
     Tensor o = out_or_new(o_in, q.sizes(), dt, q);
     OptTensor so = state_out_in;
     if (!so && want_state) so = new_empty(dim.state, at::kFloat, q);
-    const Workspace ws = decay_workspace(need, ws_in, q, to);
+    const Workspace ws = decay_workspace(marks ? 0 : need.forward, ws_in, q, to);
     check(lib.decay_forward(&s, dev(q, "q"), dev(k, "k", dt, q.sizes()), dev(v, "v", dt, q.sizes()),
                             cf32(dev(log_decay, "log_decay", at::kFloat, dim.heads)),
                             ci32(dev(lengths, "lengths", at::kInt, dim.items)), cf32(dev(state, "state", at::kFloat, dim.state)),
-                            dev(o, "o", dt, q.sizes()), f32(dev(so, "state_out", at::kFloat, dim.state)), (float)scale, ws.ptr,
-                            ws.bytes, to.stream),
+                            dev(o, "o", dt, q.sizes()), f32(dev(so, "state_out", at::kFloat, dim.state)),
+                            f32(marks_ptr(marks, need.marks)), (float)scale, ws.ptr, ws.bytes, to.stream),
           "flare_decay_forward");
     return {o, so};
 }
@@ -596,26 +605,26 @@ std::tuple<Tensor, Tensor, Tensor, OptTensor> decay_backward(const Tensor &q, co
                                                              const Tensor &d_o, double scale, const OptTensor &lengths,
                                                              const OptTensor &state, const OptTensor &dstate_out,
                                                              const OptTensor &dq_in, const OptTensor &dk_in, const OptTensor &dv_in,
-                                                             const OptTensor &dstate_in, bool want_dstate, const OptTensor &ws_in,
-                                                             const py::object &stream, int layout)
+                                                             const OptTensor &dstate_in, bool want_dstate, const OptTensor &marks,
+                                                             const OptTensor &ws_in, const py::object &stream, int layout)
 {
     const OptTensor ok = k, ov = v, og = log_decay, od = d_o;
     const c10::DeviceGuard guard(one_device(
-        q, "q", {&ok, &ov, &og, &od, &lengths, &state, &dstate_out, &dq_in, &dk_in, &dv_in, &dstate_in, &ws_in}));
+        q, "q", {&ok, &ov, &og, &od, &lengths, &state, &dstate_out, &dq_in, &dk_in, &dv_in, &dstate_in, &marks, &ws_in}));
     const flare_decay_shape s = decay_shape_of(q, layout);
     const DecayDims dim(s);
     const Target to = target(stream, !ws_in);
     const py::gil_scoped_release no_gil;
     const at::ScalarType dt = q.scalar_type();
-    const size_t need = decay_bytes(s, true);
+    const DecayBytes need = decay_bytes(s);
     Tensor dq = out_or_new(dq_in, q.sizes(), dt, q), dk = out_or_new(dk_in, q.sizes(), dt, q), dv = out_or_new(dv_in, q.sizes(), dt, q);
     OptTensor ds = dstate_in;
     if (!ds && want_dstate) ds = new_empty(dim.state, at::kFloat, q);
-    const Workspace ws = decay_workspace(need, ws_in, q, to);
+    const Workspace ws = decay_workspace(need.backward, ws_in, q, to);
     check(lib.decay_backward(&s, dev(q, "q"), dev(k, "k", dt, q.sizes()), dev(v, "v", dt, q.sizes()),
                              cf32(dev(log_decay, "log_decay", at::kFloat, dim.heads)),
                              ci32(dev(lengths, "lengths", at::kInt, dim.items)), cf32(dev(state, "state", at::kFloat, dim.state)),
-                             dev(d_o, "d_o", dt, q.sizes()), cf32(dev(dstate_out, "dstate_out", at::kFloat, dim.state)),
+                             cf32(marks_ptr(marks, need.marks)), dev(d_o, "d_o", dt, q.sizes()), cf32(dev(dstate_out, "dstate_out", at::kFloat, dim.state)),
                              dev(dq, "dq", dt, q.sizes()), dev(dk, "dk", dt, q.sizes()), dev(dv, "dv", dt, q.sizes()),
                              f32(dev(ds, "dstate_in", at::kFloat, dim.state)), (float)scale, ws.ptr, ws.bytes, to.stream),
           "flare_decay_backward");
@@ -649,7 +658,8 @@ Tensor decay_step(const Tensor &q, const Tensor &k, const Tensor &v, const Tenso
 }
 
 struct DecayBackward : torch::autograd::Node {
-    torch::autograd::SavedVariable q, k, v, log_decay, lengths, state;
+    torch::autograd::SavedVariable q, k, v, log_decay, lengths, state, marks;
+    bool has_marks = false;
     flare_decay_shape shape{};
     float scale = 0.f;
 
@@ -657,7 +667,7 @@ struct DecayBackward : torch::autograd::Node {
     void release_variables() override
     {
         std::lock_guard<std::mutex> lock(mutex_);
-        for (auto *t : {&q, &k, &v, &log_decay, &lengths, &state}) t->reset_data();
+        for (auto *t : {&q, &k, &v, &log_decay, &lengths, &state, &marks}) t->reset_data();
     }
     torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override
     {
@@ -667,7 +677,7 @@ struct DecayBackward : torch::autograd::Node {
     torch::autograd::variable_list gradients(Tensor &&d_o, Tensor &&dstate)
     {
         const Tensor tq = q.unpack(), tk = k.unpack(), tv = v.unpack(), tg = log_decay.unpack();
-        const OptTensor tl = defined(lengths.unpack()), ts = defined(state.unpack());
+        const OptTensor tl = defined(lengths.unpack()), ts = defined(state.unpack()), tm = defined(marks.unpack());
         // held against the forward's shape, as a saved-tensor hook may have handed back anything
         const at::ScalarType dt = scalar_type(shape.dtype);
         const bool heads_first = shape.layout == FLARE_BHND;
@@ -676,16 +686,19 @@ struct DecayBackward : torch::autograd::Node {
         const void *const pq = dev(tq, "q", dt, tok), *const pk = dev(tk, "k", dt, tok), *const pv = dev(tv, "v", dt, tok),
                    *const pg = dev(tg, "log_decay", at::kFloat, dim.heads), *const pl = dev(tl, "lengths", at::kInt, dim.items),
                    *const ps = dev(ts, "state", at::kFloat, dim.state);
+        const DecayBytes need = decay_bytes(shape);
+        if (tm.has_value() != has_marks) throw Error("a saved tensor is missing");
+        const void *const pm = marks_ptr(tm, need.marks);
         const OptTensor ok = tk, ov = tv, og = tg;
-        const c10::DeviceGuard guard(one_device(tq, "q", {&ok, &ov, &og, &tl, &ts}));
+        const c10::DeviceGuard guard(one_device(tq, "q", {&ok, &ov, &og, &tl, &ts, &tm}));
         if (!d_o.defined()) d_o = at::zeros(tok, tq.options().requires_grad(false));   // only the state was used
         d_o = d_o.contiguous();
         OptTensor ds = contiguous(defined(dstate));
         const Target to{c10::hip::getCurrentHIPStream().stream(), std::nullopt};
         Tensor dq = new_empty(tok, dt, tq), dk = new_empty(tok, dt, tq), dv = new_empty(tok, dt, tq), dfirst;
         if (ts && task_should_compute_output(3)) dfirst = new_empty(dim.state, at::kFloat, tq);
-        const Workspace ws = decay_workspace(decay_bytes(shape, true), std::nullopt, tq, to);
-        check(lib.decay_backward(&shape, pq, pk, pv, cf32(pg), ci32(pl), cf32(ps), dev(d_o, "the gradient of o", dt, tok),
+        const Workspace ws = decay_workspace(need.backward, std::nullopt, tq, to);
+        check(lib.decay_backward(&shape, pq, pk, pv, cf32(pg), ci32(pl), cf32(ps), cf32(pm), dev(d_o, "the gradient of o", dt, tok),
                                  cf32(dev(ds, "the gradient of the state", at::kFloat, dim.state)), dq.data_ptr(), dk.data_ptr(),
                                  dv.data_ptr(), dfirst.defined() ? f32(dfirst.data_ptr()) : nullptr, scale, ws.ptr, ws.bytes,
                                  to.stream),
@@ -726,14 +739,16 @@ std::optional<std::tuple<Tensor, OptTensor>> decay_mixer(const Tensor &q_in, con
     const DecayDims dim(s);
     const at::ScalarType dt = q.scalar_type();
     const Target to{c10::hip::getCurrentHIPStream().stream(), std::nullopt};
-    const size_t need = decay_bytes(s, false);
-    Tensor o = new_empty(q.sizes(), dt, q), state_out;
+    const DecayBytes need = decay_bytes(s);
+    Tensor o = new_empty(q.sizes(), dt, q), state_out, marks;
     if (want_state) state_out = new_empty(dim.state, at::kFloat, q);
-    const Workspace ws = decay_workspace(need, std::nullopt, q, to);
+    if (node && need.marks) marks = new_empty({(int64_t)(need.marks / 4)}, at::kFloat, q);
+    const Workspace ws = decay_workspace(marks.defined() ? 0 : need.forward, std::nullopt, q, to);
     check(lib.decay_forward(&s, dev(q, "q"), dev(k, "k", dt, q.sizes()), dev(v, "v", dt, q.sizes()),
                             cf32(dev(log_decay, "log_decay", at::kFloat, dim.heads)),
                             ci32(dev(lengths, "lengths", at::kInt, dim.items)), cf32(dev(state, "state", at::kFloat, dim.state)),
-                            o.data_ptr(), want_state ? f32(state_out.data_ptr()) : nullptr, (float)scale, ws.ptr, ws.bytes, to.stream),
+                            o.data_ptr(), want_state ? f32(state_out.data_ptr()) : nullptr,
+                            marks.defined() ? f32(marks.data_ptr()) : nullptr, (float)scale, ws.ptr, ws.bytes, to.stream),
           "flare_decay_forward");
     if (node) {
         node->shape = s;
@@ -744,6 +759,8 @@ std::optional<std::tuple<Tensor, OptTensor>> decay_mixer(const Tensor &q_in, con
         node->log_decay = torch::autograd::SavedVariable(log_decay, false);
         node->lengths = torch::autograd::SavedVariable(or_none(lengths), false);
         node->state = torch::autograd::SavedVariable(or_none(state), false);
+        node->marks = torch::autograd::SavedVariable(marks, false);
+        node->has_marks = marks.defined();
         torch::autograd::set_history(o, node);
         if (want_state) torch::autograd::set_history(state_out, node);
     }

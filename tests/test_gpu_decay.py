@@ -103,7 +103,8 @@ def test_forward_and_backward(B, H, N, d, dtype, layout, lengths, state):
             size = size + 2.0 ** -14 * size.max()           # a weight times a subnormal d_o
         check(name, back(got, layout if tok else "bhnd"), want, size, dtype if tok or dtype == "f16" else "f32", N, d, 2 if tok else 1)
     # the same bits again, and with a workspace and outputs of the caller's (the state over the one that came in, o over q)
-    f_bytes, b_bytes = binding.decay_workspace_bytes(B, H, N, d, binding._dtype_code(dev["q"]), layout)
+    f_bytes, b_bytes, m_bytes = binding.decay_workspace_bytes(B, H, N, d, binding._dtype_code(dev["q"]), layout)
+    marks = torch.full((m_bytes // 4,), float("nan"), device="cuda")
     ws = torch.full((max(f_bytes, b_bytes, 256),), 0xFF, dtype=torch.uint8, device="cuda")
     again = binding.decay_backward(*args, dev["d_o"], scale, dstate_out=dev["dstate_out"], want_dstate=True, workspace=ws, **keep)
     assert all(torch.equal(a, b) for a, b in zip(again, (dq, dk, dv, ds)))
@@ -112,6 +113,10 @@ def test_forward_and_backward(B, H, N, d, dtype, layout, lengths, state):
     keep["state"] = carried
     o2, s2 = binding.decay_forward(over, *args[1:], scale, o=over, state_out=carried, want_state=True, workspace=ws, **keep)
     assert o2 is over and torch.equal(o2, o) and torch.equal(s2, s)
+    keep["state"] = dev["state"]
+    binding.decay_forward(*args, scale, marks=marks, **keep)
+    again = binding.decay_backward(*args, dev["d_o"], scale, dstate_out=dev["dstate_out"], want_dstate=True, marks=marks, **keep)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dq, dk, dv, ds)))
     if lengths is not None:      # padding is zeros
         for t in (o, dq, dk, dv):
             for b in range(B):
@@ -204,18 +209,19 @@ def test_step(B, H, d, dtype):
     assert torch.equal(o2[on], o[on]) and (o2[~on] == 0).all()
 
 
-def test_fp16_beyond_its_range():
-    """A state above 65504 and gradients among the subnormals: neither may overflow, or be lost, inside."""
+@pytest.mark.parametrize("q_size,kv_size,g_size", [(2.0 ** -10, 256.0, 2.0 ** -18), (1024.0, 2.0 ** -9, 2.0 ** -8)])
+def test_fp16_beyond_its_range(q_size, kv_size, g_size):
+    """A state above 65504, or one among the subnormals, and such gradients: nothing may overflow, or be lost, inside."""
     B, H, N, d = 1, 2, 500, 32
-    print("[case] fp16 range", flush=True)
+    print("[case] fp16 range %g" % kv_size, flush=True)
     dev, wide = make(B, H, N, d, "f16", 13, decays=[0.0, -0.001])
-    for n, f in (("q", 2.0 ** -10), ("k", 256.0), ("v", 256.0), ("d_o", 2.0 ** -18)):
+    for n, f in (("q", q_size), ("k", kv_size), ("v", kv_size), ("d_o", g_size)):
         dev[n] = (dev[n] * f).contiguous()
         wide[n] = dev[n].double().cpu()
     args = [dev[n] for n in ("q", "k", "v", "log_decay")]
     want, size = (_plain.decay(t["q"], t["k"], t["v"], t["log_decay"], 2.0 ** -6) for t in (wide, magnitudes(wide)))
     o, s = binding.decay_forward(*args, 2.0 ** -6, want_state=True)
-    assert s.abs().max() > 65504
+    assert s.abs().max() > 65504 or s.abs().max() < 2.0 ** -10
     check("o", back(o, "bhnd"), want[0], size[0], "f16", N, d, 2)
     check("state", back(s, "bhnd"), want[1], size[1], "f16", N, d, 1)
     grads = binding.decay_backward(*args, dev["d_o"], 2.0 ** -6)
@@ -336,9 +342,9 @@ def test_other_stream_and_graph():
     dev, _ = make(B, H, N, d, "bf16", 31, lengths=[700, 400], state=True)
     args = [dev[n] for n in ("q", "k", "v", "log_decay")]
     tok = [dev[n][:, :, 5].contiguous() for n in ("q", "k", "v")]
-    f_bytes, b_bytes = binding.decay_workspace_bytes(B, H, N, d, binding.FLARE_BF16)
-    assert f_bytes > 0 and b_bytes > f_bytes
-    ws = torch.empty(b_bytes, dtype=torch.uint8, device="cuda")
+    f_bytes, b_bytes, _ = binding.decay_workspace_bytes(B, H, N, d, binding.FLARE_BF16)
+    assert f_bytes > 0 and b_bytes > 0
+    ws = torch.empty(max(f_bytes, b_bytes), dtype=torch.uint8, device="cuda")
 
     def run(o, stream=None, workspace=None):
         keep = dict(lengths=dev["lengths"], state=dev["state"], workspace=workspace, stream=stream)

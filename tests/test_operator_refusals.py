@@ -18,39 +18,40 @@ def lib():
 def test_decay_shapes(lib):
     good = (2, 3, 100, 64, binding.FLARE_BF16, 0)
     f, b = ctypes.c_size_t(1), ctypes.c_size_t(1)
-    assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*good)), ctypes.byref(f), ctypes.byref(b)) == 0
-    assert lib.flare_decay_workspace_bytes(None, None, None) == -1
+    assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*good)), ctypes.byref(f), ctypes.byref(b), None) == 0
+    assert lib.flare_decay_workspace_bytes(None, None, None, None) == -1
     bad = [(0, 3, 100, 64, 1, 0, -1), (2, 0, 100, 64, 1, 0, -1), (2, 3, 0, 64, 1, 0, -1), (2, 3, 100, 0, 1, 0, -1),
            (2, 3, 100, 48, 1, 0, -2), (2, 3, 100, 256, 1, 0, -2), (2, 3, 100, 8, 1, 0, -2), (2, 3, 100, 64, 3, 0, -2),
            (2, 3, 100, 64, 1, 2, -2), (70000, 1, 100, 64, 1, 0, -2), (1, 1, 1 << 24, 16, 1, 0, -2), (1, 300, 1 << 20, 128, 1, 1, -2)]
     for *shape, code in bad:
-        assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*shape)), None, None) == code, shape
+        assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*shape)), None, None, None) == code, shape
 
 
 def test_decay_arguments(lib):
     one = ctypes.byref(DecayShape(1, 2, 40, 64, binding.FLARE_F16, 0))
-    args = [P, P, P, P, None, None, P, None]
+    args = [P, P, P, P, None, None, P, None, None]
     for i in (0, 1, 2, 3, 6):
         a = list(args)
         a[i] = None
         assert lib.flare_decay_forward(one, *a, ONE, None, 0, None) == -1
-    for i in range(8):
+    for i in range(9):
         a = list(args)
         a[i] = ODD
         assert lib.flare_decay_forward(one, *a, ONE, None, 0, None) == -3
-    back = [P, P, P, P, None, None, P, None, P, P, P, None]
-    for i in (0, 1, 2, 3, 6, 8, 9, 10):
+    back = [P, P, P, P, None, None, None, P, None, P, P, P, None]
+    for i in (0, 1, 2, 3, 7, 9, 10, 11):
         a = list(back)
         a[i] = None
         assert lib.flare_decay_backward(one, *a, ONE, None, 0, None) == -1
-    for i in range(12):
+    for i in range(13):
         a = list(back)
         a[i] = ODD
         assert lib.flare_decay_backward(one, *a, ONE, None, 0, None) == -3
     # a long sequence of few heads is split, and needs its slots
     long = DecayShape(1, 1, 100000, 128, binding.FLARE_BF16, 0)
-    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    assert lib.flare_decay_workspace_bytes(ctypes.byref(long), ctypes.byref(f), ctypes.byref(b)) == 0 and f.value and b.value
+    f, b, m = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    assert lib.flare_decay_workspace_bytes(ctypes.byref(long), ctypes.byref(f), ctypes.byref(b), ctypes.byref(m)) == 0
+    assert f.value and b.value and m.value
     assert lib.flare_decay_forward(ctypes.byref(long), *args, ONE, None, 0, None) == -4
     assert lib.flare_decay_forward(ctypes.byref(long), *args, ONE, P, f.value - 1, None) == -4
     assert lib.flare_decay_forward(ctypes.byref(long), *args, ONE, ODD, f.value, None) == -3
