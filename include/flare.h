@@ -287,8 +287,9 @@ typedef struct {
 } flare_decay_shape;
 
 /* Scratch bytes of flare_decay_forward and flare_decay_backward without marks (with them never more; the forward then
- * needs none), and the size of marks; each pointer may be NULL, each number 0.  Host-only. */
-int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes, size_t *marks_bytes);
+ * needs none), and the size of marks, for calls with lengths (padded) or without; each pointer may be NULL, each number 0.
+ * Host-only. */
+int flare_decay_workspace_bytes(const flare_decay_shape *shape, int padded, size_t *fwd_bytes, size_t *bwd_bytes, size_t *marks_bytes);
 
 /*
  *   q, k, v, log_decay, lengths (or NULL), state_in (or NULL: zero)                                       (in)

@@ -90,7 +90,7 @@ def load():
     lib.flare_spectral.argtypes = [sp, vp, vp, fp, fp, ctypes.c_float, ctypes.c_int, fp, fp, fp, vp, ctypes.c_size_t, vp]
     size, dp, np = ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(DecayShape), ctypes.POINTER(NormShape)
     pp, f = ctypes.POINTER(NormParams), ctypes.c_float
-    lib.flare_decay_workspace_bytes.argtypes = [dp, size, size, size]
+    lib.flare_decay_workspace_bytes.argtypes = [dp, ctypes.c_int, size, size, size]
     lib.flare_decay_forward.argtypes = [dp, vp, vp, vp, fp, vp, fp, vp, fp, fp, f, vp, ctypes.c_size_t, vp]
     lib.flare_decay_backward.argtypes = [dp, vp, vp, vp, fp, vp, fp, fp, vp, fp, vp, vp, vp, fp, f, vp, ctypes.c_size_t, vp]
     lib.flare_decay_step.argtypes = [dp, vp, vp, vp, fp, vp, fp, fp, vp, f, vp]
@@ -285,11 +285,12 @@ def spectral(q_lat, k, lse_enc, lse_dec, scale, first=0, want_gram=False, stream
 
 
 # ---- decay mixer -----------------------------------------------------------------------------------------------------
-def decay_workspace_bytes(B, H, N, d, dtype_code, layout="bhnd"):
-    """(forward bytes, backward bytes, bytes of marks) of the decay mixer for this shape; each may be 0."""
+def decay_workspace_bytes(B, H, N, d, dtype_code, layout="bhnd", padded=False):
+    """(forward bytes, backward bytes, bytes of marks) of the decay mixer for this shape, with lengths (padded) or without;
+    each may be 0."""
     shp = DecayShape(B, H, N, d, dtype_code, _layout(layout))
     f, b, m = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
-    _check(load().flare_decay_workspace_bytes(ctypes.byref(shp), ctypes.byref(f), ctypes.byref(b), ctypes.byref(m)),
+    _check(load().flare_decay_workspace_bytes(ctypes.byref(shp), 1 if padded else 0, ctypes.byref(f), ctypes.byref(b), ctypes.byref(m)),
            "flare_decay_workspace_bytes")
     return int(f.value), int(b.value), int(m.value)
 

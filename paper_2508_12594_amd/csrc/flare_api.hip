@@ -340,13 +340,13 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
                         static_cast<hipStream_t>(stream));
 }
 
-int flare_decay_workspace_bytes(const flare_decay_shape *shape, size_t *fwd_bytes, size_t *bwd_bytes, size_t *marks_bytes)
+int flare_decay_workspace_bytes(const flare_decay_shape *shape, int padded, size_t *fwd_bytes, size_t *bwd_bytes, size_t *marks_bytes)
 {
     const int rc = check_decay(shape);
     if (rc != FLARE_OK) return rc;
-    if (fwd_bytes) *fwd_bytes = decay_fwd_bytes(*shape, false);
-    if (bwd_bytes) *bwd_bytes = decay_bwd_bytes(*shape, false);
-    if (marks_bytes) *marks_bytes = decay_marks_bytes(*shape);
+    if (fwd_bytes) *fwd_bytes = decay_fwd_bytes(*shape, padded, false);
+    if (bwd_bytes) *bwd_bytes = decay_bwd_bytes(*shape, padded, false);
+    if (marks_bytes) *marks_bytes = decay_marks_bytes(*shape, padded);
     return FLARE_OK;
 }
 
@@ -360,7 +360,7 @@ int flare_decay_forward(const flare_decay_shape *shape, const void *q, const voi
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(lengths) ||
         !aligned16(state_in) || !aligned16(o) || !aligned16(state_out) || !aligned16(marks) || !aligned16(workspace))
         return FLARE_EALIGN;
-    const size_t need = decay_fwd_bytes(*shape, marks != nullptr);
+    const size_t need = decay_fwd_bytes(*shape, lengths != nullptr, marks != nullptr);
     if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
     return decay_forward(*shape, q, k, v, log_decay, lengths, state_in, o, state_out, marks, scale, workspace,
                          static_cast<hipStream_t>(stream));
@@ -377,7 +377,7 @@ int flare_decay_backward(const flare_decay_shape *shape, const void *q, const vo
         !aligned16(state_in) || !aligned16(marks) || !aligned16(d_o) || !aligned16(dstate_out) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
         !aligned16(dstate_in) || !aligned16(workspace))
         return FLARE_EALIGN;
-    const size_t need = decay_bwd_bytes(*shape, marks != nullptr);
+    const size_t need = decay_bwd_bytes(*shape, lengths != nullptr, marks != nullptr);
     if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
     return decay_backward(*shape, q, k, v, log_decay, lengths, state_in, marks, d_o, dstate_out, dq, dk, dv, dstate_in, scale, workspace,
                           static_cast<hipStream_t>(stream));

@@ -197,9 +197,10 @@ int spectral_run(const flare_shape &s, const void *q, const void *k, const float
                  float scale, int first, float *evals, float *zvec, float *gram, void *ws, hipStream_t stream);
 
 // ---- decay mixer (flare_decay.hip); state_in, lengths, marks, state_out, dstate_* and active may be NULL ----------
-size_t decay_marks_bytes(const flare_decay_shape &s);
-size_t decay_fwd_bytes(const flare_decay_shape &s, bool marks);    // marks: are they written (read)?
-size_t decay_bwd_bytes(const flare_decay_shape &s, bool marks);
+// padded: are there lengths?  marks: are they written (read)?
+size_t decay_marks_bytes(const flare_decay_shape &s, bool padded);
+size_t decay_fwd_bytes(const flare_decay_shape &s, bool padded, bool marks);
+size_t decay_bwd_bytes(const flare_decay_shape &s, bool padded, bool marks);
 int decay_forward(const flare_decay_shape &s, const void *q, const void *k, const void *v, const float *log_decay,
                   const int *lengths, const float *state_in, void *o, float *state_out, float *marks, float scale, void *ws,
                   hipStream_t stream);

@@ -553,10 +553,10 @@ flare_decay_shape decay_shape_of(const Tensor &q, int layout)
 const float *cf32(const void *p) { return static_cast<const float *>(p); }
 const int *ci32(const void *p) { return static_cast<const int *>(p); }
 struct DecayBytes { size_t forward = 0, backward = 0, marks = 0; };
-DecayBytes decay_bytes(const flare_decay_shape &s)
+DecayBytes decay_bytes(const flare_decay_shape &s, bool padded)
 {
     DecayBytes n;
-    check(lib.decay_workspace_bytes(&s, &n.forward, &n.backward, &n.marks), "flare_decay_workspace_bytes");
+    check(lib.decay_workspace_bytes(&s, padded, &n.forward, &n.backward, &n.marks), "flare_decay_workspace_bytes");
     return n;
 }
 // marks that the caller brought: fp32, of any shape
@@ -587,7 +587,7 @@ std::tuple<Tensor, OptTensor> decay_forward(const Tensor &q, const Tensor &k, co
     const Target to = target(stream, !ws_in);
     const py::gil_scoped_release no_gil;
     const at::ScalarType dt = q.scalar_type();
-    const DecayBytes need = decay_bytes(s);
+    const DecayBytes need = decay_bytes(s, lengths.has_value());
     Tensor o = out_or_new(o_in, q.sizes(), dt, q);
     OptTensor so = state_out_in;
     if (!so && want_state) so = new_empty(dim.state, at::kFloat, q);
@@ -616,7 +616,7 @@ std::tuple<Tensor, Tensor, Tensor, OptTensor> decay_backward(const Tensor &q, co
     const Target to = target(stream, !ws_in);
     const py::gil_scoped_release no_gil;
     const at::ScalarType dt = q.scalar_type();
-    const DecayBytes need = decay_bytes(s);
+    const DecayBytes need = decay_bytes(s, lengths.has_value());
     Tensor dq = out_or_new(dq_in, q.sizes(), dt, q), dk = out_or_new(dk_in, q.sizes(), dt, q), dv = out_or_new(dv_in, q.sizes(), dt, q);
     OptTensor ds = dstate_in;
     if (!ds && want_dstate) ds = new_empty(dim.state, at::kFloat, q);
@@ -686,7 +686,7 @@ struct DecayBackward : torch::autograd::Node {
         const void *const pq = dev(tq, "q", dt, tok), *const pk = dev(tk, "k", dt, tok), *const pv = dev(tv, "v", dt, tok),
                    *const pg = dev(tg, "log_decay", at::kFloat, dim.heads), *const pl = dev(tl, "lengths", at::kInt, dim.items),
                    *const ps = dev(ts, "state", at::kFloat, dim.state);
-        const DecayBytes need = decay_bytes(shape);
+        const DecayBytes need = decay_bytes(shape, tl.has_value());
         if (tm.has_value() != has_marks) throw Error("a saved tensor is missing");
         const void *const pm = marks_ptr(tm, need.marks);
         const OptTensor ok = tk, ov = tv, og = tg;
@@ -739,7 +739,7 @@ std::optional<std::tuple<Tensor, OptTensor>> decay_mixer(const Tensor &q_in, con
     const DecayDims dim(s);
     const at::ScalarType dt = q.scalar_type();
     const Target to{c10::hip::getCurrentHIPStream().stream(), std::nullopt};
-    const DecayBytes need = decay_bytes(s);
+    const DecayBytes need = decay_bytes(s, lengths.has_value());
     Tensor o = new_empty(q.sizes(), dt, q), state_out, marks;
     if (want_state) state_out = new_empty(dim.state, at::kFloat, q);
     if (node && need.marks) marks = new_empty({(int64_t)(need.marks / 4)}, at::kFloat, q);

@@ -103,7 +103,8 @@ def test_forward_and_backward(B, H, N, d, dtype, layout, lengths, state):
             size = size + 2.0 ** -14 * size.max()           # a weight times a subnormal d_o
         check(name, back(got, layout if tok else "bhnd"), want, size, dtype if tok or dtype == "f16" else "f32", N, d, 2 if tok else 1)
     # the same bits again, and with a workspace and outputs of the caller's (the state over the one that came in, o over q)
-    f_bytes, b_bytes, m_bytes = binding.decay_workspace_bytes(B, H, N, d, binding._dtype_code(dev["q"]), layout)
+    f_bytes, b_bytes, m_bytes = binding.decay_workspace_bytes(B, H, N, d, binding._dtype_code(dev["q"]), layout,
+                                                               padded=lengths is not None)
     marks = torch.full((m_bytes // 4,), float("nan"), device="cuda")
     ws = torch.full((max(f_bytes, b_bytes, 256),), 0xFF, dtype=torch.uint8, device="cuda")
     again = binding.decay_backward(*args, dev["d_o"], scale, dstate_out=dev["dstate_out"], want_dstate=True, workspace=ws, **keep)
@@ -342,7 +343,7 @@ def test_other_stream_and_graph():
     dev, _ = make(B, H, N, d, "bf16", 31, lengths=[700, 400], state=True)
     args = [dev[n] for n in ("q", "k", "v", "log_decay")]
     tok = [dev[n][:, :, 5].contiguous() for n in ("q", "k", "v")]
-    f_bytes, b_bytes, _ = binding.decay_workspace_bytes(B, H, N, d, binding.FLARE_BF16)
+    f_bytes, b_bytes, _ = binding.decay_workspace_bytes(B, H, N, d, binding.FLARE_BF16, padded=True)
     assert f_bytes > 0 and b_bytes > 0
     ws = torch.empty(max(f_bytes, b_bytes), dtype=torch.uint8, device="cuda")
 

@@ -18,13 +18,13 @@ def lib():
 def test_decay_shapes(lib):
     good = (2, 3, 100, 64, binding.FLARE_BF16, 0)
     f, b = ctypes.c_size_t(1), ctypes.c_size_t(1)
-    assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*good)), ctypes.byref(f), ctypes.byref(b), None) == 0
-    assert lib.flare_decay_workspace_bytes(None, None, None, None) == -1
+    assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*good)), 0, ctypes.byref(f), ctypes.byref(b), None) == 0
+    assert lib.flare_decay_workspace_bytes(None, 0, None, None, None) == -1
     bad = [(0, 3, 100, 64, 1, 0, -1), (2, 0, 100, 64, 1, 0, -1), (2, 3, 0, 64, 1, 0, -1), (2, 3, 100, 0, 1, 0, -1),
            (2, 3, 100, 48, 1, 0, -2), (2, 3, 100, 256, 1, 0, -2), (2, 3, 100, 8, 1, 0, -2), (2, 3, 100, 64, 3, 0, -2),
            (2, 3, 100, 64, 1, 2, -2), (70000, 1, 100, 64, 1, 0, -2), (1, 1, 1 << 24, 16, 1, 0, -2), (1, 300, 1 << 20, 128, 1, 1, -2)]
     for *shape, code in bad:
-        assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*shape)), None, None, None) == code, shape
+        assert lib.flare_decay_workspace_bytes(ctypes.byref(DecayShape(*shape)), 0, None, None, None) == code, shape
 
 
 def test_decay_arguments(lib):
@@ -50,7 +50,7 @@ def test_decay_arguments(lib):
     # a long sequence of few heads is split, and needs its slots
     long = DecayShape(1, 1, 100000, 128, binding.FLARE_BF16, 0)
     f, b, m = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
-    assert lib.flare_decay_workspace_bytes(ctypes.byref(long), ctypes.byref(f), ctypes.byref(b), ctypes.byref(m)) == 0
+    assert lib.flare_decay_workspace_bytes(ctypes.byref(long), 0, ctypes.byref(f), ctypes.byref(b), ctypes.byref(m)) == 0
     assert f.value and b.value and m.value
     assert lib.flare_decay_forward(ctypes.byref(long), *args, ONE, None, 0, None) == -4
     assert lib.flare_decay_forward(ctypes.byref(long), *args, ONE, P, f.value - 1, None) == -4
