@@ -659,7 +659,7 @@ Tensor decay_step(const Tensor &q, const Tensor &k, const Tensor &v, const Tenso
 
 struct DecayBackward : torch::autograd::Node {
     torch::autograd::SavedVariable q, k, v, log_decay, lengths, state, marks;
-    bool has_marks = false;
+    bool has_marks = false, has_lengths = false;
     flare_decay_shape shape{};
     float scale = 0.f;
 
@@ -687,7 +687,7 @@ struct DecayBackward : torch::autograd::Node {
                    *const pg = dev(tg, "log_decay", at::kFloat, dim.heads), *const pl = dev(tl, "lengths", at::kInt, dim.items),
                    *const ps = dev(ts, "state", at::kFloat, dim.state);
         const DecayBytes need = decay_bytes(shape, tl.has_value());
-        if (tm.has_value() != has_marks) throw Error("a saved tensor is missing");
+        if (tm.has_value() != has_marks || tl.has_value() != has_lengths) throw Error("a saved tensor is missing");
         const void *const pm = marks_ptr(tm, need.marks);
         const OptTensor ok = tk, ov = tv, og = tg;
         const c10::DeviceGuard guard(one_device(tq, "q", {&ok, &ov, &og, &tl, &ts, &tm}));
@@ -761,6 +761,7 @@ std::optional<std::tuple<Tensor, OptTensor>> decay_mixer(const Tensor &q_in, con
         node->state = torch::autograd::SavedVariable(or_none(state), false);
         node->marks = torch::autograd::SavedVariable(marks, false);
         node->has_marks = marks.defined();
+        node->has_lengths = lengths.has_value();
         torch::autograd::set_history(o, node);
         if (want_state) torch::autograd::set_history(state_out, node);
     }
