@@ -163,7 +163,8 @@ __device__ __forceinline__ void load_param(const float *w, float otherwise, int 
         for (int i = 0; i < 8; ++i) v[i] = otherwise;
     }
 }
-__device__ __forceinline__ float sigmoid(float g) { return 1.f / (1.f + __expf(-g)); }
+// (v_exp_f32 and v_rcp_f32: a few steps of 2^-24.  An exponential that overflows has the reciprocal 0.)
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(-kLog2e * g)); }
 __device__ __forceinline__ float act_of(int act, float g)
 {
     return act == FLARE_GATE_PLAIN ? g : act == FLARE_GATE_SIGMOID ? sigmoid(g) : g * sigmoid(g);
@@ -180,7 +181,7 @@ __device__ __forceinline__ void row_stats(const float (&v)[8], int kind, int l, 
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[0] += v[i];          // (zero beyond C)
         row_sum<LPR>(s, red, turn);
-        mean = s[0] / (float)C;
+        mean = s[0] * (1.f / (float)C);
     }
     s[0] = 0.f;
 #pragma unroll
@@ -189,7 +190,7 @@ __device__ __forceinline__ void row_stats(const float (&v)[8], int kind, int l, 
         s[0] = fmaf(t, t, s[0]);
     }
     row_sum<LPR>(s, red, turn);
-    scale = 1.f / sqrtf(s[0] / (float)C + eps);
+    scale = 1.f / sqrtf(s[0] * (1.f / (float)C) + eps);
 }
 
 // RICH: there is a post norm or a gate.
@@ -285,69 +286,105 @@ __global__ __launch_bounds__(Lanes<LPR>::THREADS) void residual_norm_backward_ke
     __shared__ float slots[L::ROWS > 1 ? L::ROWS * 8 * LPR : 1];
     const int l = threadIdx.x % LPR, slot = threadIdx.x / LPR, C = a.C;
     int turn = 0;
+    // 1024 lanes have 128 registers each: no room for the weights, nor for a row asked for ahead (two rows ahead are no faster), and
+    // with a post norm or a gate the sums over the rows lie in LDS (4096 rows of 8192 channels: 447 us with them spilled).
+    constexpr bool KEEP = LPR < 1024, SUMS_IN_LDS = LPR == 1024 && RICH;
+    __shared__ float4 lds_sums[SUMS_IN_LDS ? 4 * 2 * LPR : 1];
+    const auto add_in_lds = [&](int which, const float (&v)[8]) {
+        if (!(a.want >> which & 1)) return;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float4 &t = lds_sums[(2 * which + k) * LPR + l];
+            t = make_float4(t.x + v[4 * k], t.y + v[4 * k + 1], t.z + v[4 * k + 2], t.w + v[4 * k + 3]);
+        }
+    };
+    if constexpr (SUMS_IN_LDS) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) lds_sums[k * LPR + l] = make_float4(0.f, 0.f, 0.f, 0.f);    // (each lane its own)
+    }
     float pre_w_sum[8], pre_b_sum[8], post_w_sum[8], post_b_sum[8], gate_sum[8], pre_w[8], post_w[8], post_b[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) pre_w_sum[i] = pre_b_sum[i] = post_w_sum[i] = post_b_sum[i] = 0.f;
-    load_param<LPR, VEC>(a.pre_w, 1.f, l, C, pre_w);
-    if constexpr (RICH) {
-        load_param<LPR, VEC>(a.post_w, 1.f, l, C, post_w);
-        load_param<LPR, VEC>(a.post_b, 0.f, l, C, post_b);
-    }
+    const auto weights = [&]() {
+        load_param<LPR, VEC>(a.pre_w, 1.f, l, C, pre_w);
+        if constexpr (RICH) {
+            load_param<LPR, VEC>(a.post_w, 1.f, l, C, post_w);
+            load_param<LPR, VEC>(a.post_b, 0.f, l, C, post_b);
+        }
+    };
+    if constexpr (KEEP) weights();
+    const float per_channel = 1.f / (float)C;
     const bool gated = RICH && a.act != FLARE_GATE_NONE, normed = RICH && a.post != FLARE_NORM_NONE;
     const bool shared_gate = gated && a.rows_per_gate > 1;
     const long long u0 = (long long)blockIdx.x * a.units_per_block;
     const long long u1 = u0 + a.units_per_block < a.units ? u0 + a.units_per_block : a.units;
-    Raw<XT, VEC> rx{}, rd{};
-    Raw<DT, VEC> ry{}, rg{}, rh{};
-    float4 rs = make_float4(0.f, 1.f, 0.f, 1.f);
+    struct Row {
+        Raw<XT, VEC> x{}, d{};
+        Raw<DT, VEC> y{}, g{}, h{};
+        float4 stats = make_float4(0.f, 1.f, 0.f, 1.f);
+    };
+    Row ahead;
+    Raw<DT, VEC> group_gate{};
     for (long long unit = u0; unit < u1; ++unit) {
         const long long group_rows = shared_gate ? a.rows_per_gate : a.rows;
         const long long group = unit / a.units_per_group, in_group = unit % a.units_per_group * a.unit_rows;
         const long long begin = group * group_rows + in_group;
         const long long end = begin + (a.unit_rows < group_rows - in_group ? a.unit_rows : group_rows - in_group);
-        const auto ask = [&](long long row) {
+        const auto ask = [&](Row &to, long long row) {
             if (row >= end) row = end - 1;
-            if (a.dh) fetch<XT, LPR, VEC>(a.x, row, l, C, rx);
-            if (a.dx_out) fetch<XT, LPR, VEC>(a.dx_out, row, l, C, rd);
-            if (a.dh) fetch<DT, LPR, VEC>(a.dh, row, l, C, rh);
-            if (a.y) fetch<DT, LPR, VEC>(a.y, row, l, C, ry);
-            if (gated && !shared_gate) fetch<DT, LPR, VEC>(a.gate, row, l, C, rg);
-            if (a.stats) rs = *reinterpret_cast<const float4 *>(a.stats + 4 * row);
+            if (a.dh) fetch<XT, LPR, VEC>(a.x, row, l, C, to.x);
+            if (a.dx_out) fetch<XT, LPR, VEC>(a.dx_out, row, l, C, to.d);
+            if (a.dh) fetch<DT, LPR, VEC>(a.dh, row, l, C, to.h);
+            if (a.y) fetch<DT, LPR, VEC>(a.y, row, l, C, to.y);
+            if (gated && !shared_gate) fetch<DT, LPR, VEC>(a.gate, row, l, C, to.g);
+            if (a.stats) to.stats = *reinterpret_cast<const float4 *>(a.stats + 4 * row);
         };
-        if (shared_gate) fetch<DT, LPR, VEC>(a.gate, group, l, C, rg);
+        if (shared_gate) fetch<DT, LPR, VEC>(a.gate, group, l, C, group_gate);
 #pragma unroll
         for (int i = 0; i < 8; ++i) gate_sum[i] = 0.f;
-        ask(begin + slot);
-        for (long long row0 = begin; row0 < end; row0 += L::ROWS) {
+        const auto work_on = [&](Row &here, long long row0) {
             const long long row = row0 + slot;
             const bool live = row < end;
             float x[8], y[8], gx[8], g[8], dh[8];
-            values<XT, VEC>(rx, x);
-            values<XT, VEC>(rd, gx);
-            values<DT, VEC>(rh, dh);
-            values<DT, VEC>(ry, y);
-            if constexpr (RICH) values<DT, VEC>(rg, g);
-            const float4 st = rs;
-            if (row0 + L::ROWS < end) ask(row + L::ROWS);
+            if constexpr (!KEEP) weights();
+            values<XT, VEC>(here.x, x);
+            values<XT, VEC>(here.d, gx);
+            values<DT, VEC>(here.h, dh);
+            values<DT, VEC>(here.y, y);
+            if constexpr (RICH) values<DT, VEC>(shared_gate ? group_gate : here.g, g);
+            const float4 st = here.stats;
+            if (KEEP && row0 + L::ROWS < end) ask(here, row + L::ROWS);
             if (normed) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[i] = (y[i] - st.z) * st.w;        // the normalised branch
             }
             const auto branch = [&](int i) { return RICH ? fmaf(y[i], post_w[i], post_b[i]) : y[i]; };   // u (weights 1, 0 without a norm)
+            float act[8];                       // the gate's value; g becomes its slope
+            if (gated) {
+                if (a.act == FLARE_GATE_PLAIN) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { act[i] = g[i]; g[i] = 1.f; }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float sg = sigmoid(g[i]), rest = 1.f - sg;
+                        act[i] = a.act == FLARE_GATE_SIGMOID ? sg : g[i] * sg;
+                        g[i] = a.act == FLARE_GATE_SIGMOID ? sg * rest : sg * fmaf(g[i], rest, 1.f);
+                    }
+                }
+            }
             if (a.dh) {
                 if (a.y) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float u = branch(i);
-                        if (gated) u *= act_of(a.act, g[i]);
-                        x[i] = fmaf(a.alpha, u, x[i]);
-                    }
+                    for (int i = 0; i < 8; ++i) x[i] = fmaf(a.alpha, gated ? branch(i) * act[i] : branch(i), x[i]);
                 }
                 float s[2] = {0.f, 0.f};
+                if constexpr (SUMS_IN_LDS) add_in_lds(1, dh);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     x[i] = (x[i] - st.x) * st.y;
-                    if (live) {
+                    if constexpr (SUMS_IN_LDS) pre_w_sum[i] = dh[i] * x[i];
+                    else if (live) {
                         pre_w_sum[i] = fmaf(dh[i], x[i], pre_w_sum[i]);
                         pre_b_sum[i] += dh[i];
                     }
@@ -355,8 +392,9 @@ __global__ __launch_bounds__(Lanes<LPR>::THREADS) void residual_norm_backward_ke
                     s[0] += dh[i];
                     s[1] = fmaf(dh[i], x[i], s[1]);
                 }
+                if constexpr (SUMS_IN_LDS) add_in_lds(0, pre_w_sum);
                 row_sum<LPR>(s, red, turn);
-                const float m0 = a.pre == FLARE_NORM_LAYER ? s[0] / (float)C : 0.f, m1 = s[1] / (float)C;
+                const float m0 = a.pre == FLARE_NORM_LAYER ? s[0] * per_channel : 0.f, m1 = s[1] * per_channel;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) gx[i] += st.y * (dh[i] - m0 - x[i] * m1);
             }
@@ -368,19 +406,15 @@ __global__ __launch_bounds__(Lanes<LPR>::THREADS) void residual_norm_backward_ke
                     const bool in = channel<LPR, VEC>(l, i) < C;
                     float d = in ? a.alpha * gx[i] : 0.f;
                     if (gated) {
-                        const float u = branch(i);
-                        float act = g[i], slope = 1.f;
-                        if (a.act != FLARE_GATE_PLAIN) {
-                            const float sg = sigmoid(g[i]);
-                            act = a.act == FLARE_GATE_SIGMOID ? sg : g[i] * sg;
-                            slope = a.act == FLARE_GATE_SIGMOID ? sg * (1.f - sg) : sg * (1.f + g[i] * (1.f - sg));
-                        }
-                        const float dg = d * u * slope;
+                        const float dg = d * branch(i) * g[i];
                         if (live) gate_sum[i] = shared_gate ? gate_sum[i] + dg : dg;
-                        d *= act;
+                        d *= act[i];
                     }
                     if (normed) {
-                        if (live) {
+                        if constexpr (SUMS_IN_LDS) {
+                            post_w_sum[i] = d * y[i];
+                            post_b_sum[i] = d;
+                        } else if (live) {
                             post_w_sum[i] = fmaf(d, y[i], post_w_sum[i]);
                             post_b_sum[i] += d;
                         }
@@ -392,13 +426,22 @@ __global__ __launch_bounds__(Lanes<LPR>::THREADS) void residual_norm_backward_ke
                 }
                 if (live && a.dgate && gated && !shared_gate) store_row<DT, LPR, VEC>(a.dgate, row, l, C, gate_sum);
                 if (normed) {
+                    if constexpr (SUMS_IN_LDS) {
+                        add_in_lds(2, post_w_sum);
+                        add_in_lds(3, post_b_sum);
+                    }
                     row_sum<LPR>(s, red, turn);
-                    const float m0 = a.post == FLARE_NORM_LAYER ? s[0] / (float)C : 0.f, m1 = s[1] / (float)C;
+                    const float m0 = a.post == FLARE_NORM_LAYER ? s[0] * per_channel : 0.f, m1 = s[1] * per_channel;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) gx[i] = st.w * (gx[i] - m0 - y[i] * m1);
                 }
                 if (live && a.dy) store_row<DT, LPR, VEC>(a.dy, row, l, C, gx);
             }
+        };
+        if (KEEP) ask(ahead, begin + slot);
+        for (long long row0 = begin; row0 < end; row0 += L::ROWS) {
+            if (!KEEP) ask(ahead, row0 + slot);
+            work_on(ahead, row0);
         }
         if (shared_gate && a.dgate) {
             slot_sums<LPR>(gate_sum, slots, [&](const float (&v)[8], int lane) {
@@ -409,6 +452,16 @@ __global__ __launch_bounds__(Lanes<LPR>::THREADS) void residual_norm_backward_ke
     }
     const auto put = [&](float (&v)[8], int which) {
         if (!(a.want >> which & 1)) return;
+        if constexpr (SUMS_IN_LDS) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float4 t = lds_sums[(2 * which + k) * LPR + l];
+                v[4 * k] = t.x;
+                v[4 * k + 1] = t.y;
+                v[4 * k + 2] = t.z;
+                v[4 * k + 3] = t.w;
+            }
+        }
         slot_sums<LPR>(v, slots, [&](const float (&t)[8], int lane) {
             store_row<FLARE_F32, LPR, VEC>(a.part, (long long)blockIdx.x * 4 + which, lane, C, t);
         });
@@ -503,7 +556,7 @@ void launch_norm(const NormArgs &a, bool backward, int blocks, hipStream_t strea
     if (backward) {
         residual_norm_backward_kernel<DT, XT, LPR, VEC, RICH><<<blocks, L::THREADS, 0, stream>>>(a);
     } else {
-        const long long want = (a.rows + L::ROWS - 1) / L::ROWS, most = 1024 * 512 / L::THREADS;
+        const long long want = (a.rows + L::ROWS - 1) / L::ROWS, most = LPR <= 256 ? 8192 : 2048 * 512 / L::THREADS;
         residual_norm_kernel<DT, XT, LPR, VEC, RICH><<<(unsigned)(want < most ? want : most), L::THREADS, 0, stream>>>(a);
     }
 }
