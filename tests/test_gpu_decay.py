@@ -70,6 +70,9 @@ CASES = [  # B, H, N, d, dtype, layout, lengths, state
     (4, 3, 770, 16, "f16", "bnhd", [512, 770, 33, 513], True),
     (3, 1, 530, 32, "f32", "bhnd", [0, 530, 300], False),
     (3, 2, 290, 128, "bf16", "bnhd", [32, -5, 1000], True),
+    # more items than a wave has lanes, in segments: most of them empty, some items full, some without a token
+    (130, 2, 500, 16, "bf16", "bnhd", [(37 * b * b) % 501 if b % 5 else 0 for b in range(130)], True),
+    (70, 1, 450, 32, "f16", "bhnd", [450 if b == 69 else b % 3 for b in range(70)], True),
 ]
 
 

@@ -311,3 +311,23 @@ def test_many_rows_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(x2, x_out) and torch.equal(h2, h) and all(torch.equal(a, b) for a, b in zip(grads, grads2))
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 elements a tensor: the last rows."""
+    print("[case] norm, 8.6 GB a tensor", flush=True)
+    rows, C = (1 << 21) + 3, 2048
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, y = (torch.empty(rows, C, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(2))
+    stats = torch.empty(rows, 4, device="cuda")
+    tail = slice(rows - 5, rows)
+    x_out, h = binding.residual_norm_forward(x, y, post="rms", alpha=0.5, stats=stats)
+    small = binding.residual_norm_forward(x[tail].contiguous(), y[tail].contiguous(), post="rms", alpha=0.5)
+    assert torch.equal(x_out[tail], small[0]) and torch.equal(h[tail], small[1])
+    del h
+    grads = binding.residual_norm_backward(x, y, x_out, None, stats, post="rms", alpha=0.5)
+    small = binding.residual_norm_backward(x[tail].contiguous(), y[tail].contiguous(), x_out[tail].contiguous(), None,
+                                           stats[tail].contiguous(), post="rms", alpha=0.5)
+    assert torch.equal(grads[0][tail], small[0]) and torch.equal(grads[1][tail], small[1])
+    del x, y, x_out, grads
+    torch.cuda.empty_cache()
