@@ -17,7 +17,7 @@
 //   C   += Y^T (weight Z)  Y and Z read down their columns (transposing LDS reads), Y's columns in the order that makes the
 //                          state's registers eight neighbouring rows (state_row)
 // so that nothing but the token tiles passes through LDS.  These come by direct loads into LDS, one to three chunks ahead.
-// dK and dV share their four tiles: a workgroup of theirs has waves in two roles.
+// dK and dV share their four tiles: up to d = 64 a workgroup of theirs has waves in two roles.
 //
 // Where (b,h) are too few to fill the chip the tokens are cut into segments: a first pass takes each segment's own sum, a
 // second turns the sums into the states before the segments, a third is the scan.
@@ -73,7 +73,8 @@ struct Role {
     int turned;            // `first` and the slots hold the transposed state
 };
 struct ScanArgs {
-    const void *in[4];        // the tiles
+    const void *in[2][4];     // the tiles of either job
+    int jobs;                 // 2: neighbouring workgroups of an XCD take one job each (dK and dV, which share tiles)
     Role role[2];
     float p, w, m;            // see above
     int reverse;              // tokens from the last to the first (then lead = 0)
@@ -87,7 +88,8 @@ struct ScanArgs {
 
 constexpr float kSlow = 0x1p-16f;
 
-// SUM: a segment's own sum (tiles y, z); FORWARD: one role (x, y, z), also dQ; DKDV: two (q, k, v, dO).
+// SUM: a segment's own sum (tiles y, z); FORWARD: one role (x, y, z), also dQ, and dK and dV as two jobs; DKDV: two roles
+// (q, k, v, dO), d < 128.
 enum ScanKind { SUM = 0, FORWARD = 1, DKDV = 2 };
 
 template <int DT, int D, int KIND>
@@ -101,7 +103,7 @@ struct Scan {
     static constexpr int TILE_LOADS = BYTES / 1024;                // wave-wide loads of a tile; those of all tiles go round the waves
     static constexpr int LOADS = TILES * TILE_LOADS / WAVES;       // and so many of them are each wave's
     // Chunks held in LDS: as many as leave room for eight waves on a CU, at most four (the sums, which have least to do with a
-    // chunk; dK and dV, whose workgroup is alone on its CU).  Scans of three tiles need no more than two: 119 us, 122 with three
+    // chunk; dK and dV).  Scans of three tiles need no more than two: 119 us, 122 with three
     // (16 heads, 32768 tokens, d = 128).
     static constexpr int FIT = 160 * 1024 / (SET * (WAVES < 8 ? 8 / WAVES : 1));
     static constexpr int STAGES = FIT <= 2 || KIND == FORWARD ? 2 : FIT > 4 ? 4 : FIT;
@@ -234,13 +236,14 @@ __device__ __forceinline__ float fit_exponent(float (&v)[N], int &e)
 // Which (b,h) and segment a workgroup has.  Workgroups go round the eight XCDs: neighbouring heads whose rows share lines
 // (with [B][N][H][d]) go to one.  In a padded batch the segments that hold tokens come first, or the workgroups that have
 // anything to do would share some CUs and leave others empty (8 items of 0 to 4097 tokens, 16 heads: 151 us, 87 us like this).
-struct Work { int bh, seg; bool none; };
+struct Work { int bh, seg; bool none; int job; };
 template <int GROUP>
 __device__ __forceinline__ Work work_of(const ScanArgs &a)
 {
-    const int turn = blockIdx.x >> 3, work = (turn / GROUP * 8 + (blockIdx.x & 7)) * GROUP + turn % GROUP;
-    if (work >= a.BH * a.segments) return Work{0, 0, true};
-    if (!a.lengths) return Work{work % a.BH, work / a.BH, false};
+    const int job = a.jobs == 2 ? blockIdx.x >> 3 & 1 : 0, turn = blockIdx.x >> (a.jobs == 2 ? 4 : 3);
+    const int work = (turn / GROUP * 8 + (blockIdx.x & 7)) * GROUP + turn % GROUP;
+    if (work >= a.BH * a.segments) return Work{0, 0, true, 0};
+    if (!a.lengths) return Work{work % a.BH, work / a.BH, false, job};
     const int lane = threadIdx.x & 63, items = a.BH / a.H, h = work % a.H;
     int t = work / a.H;                        // of the segments that hold tokens (the first of an empty item, too), then of the others
     for (int other = 0; other < 2; ++other) {
@@ -259,23 +262,24 @@ __device__ __forceinline__ Work work_of(const ScanArgs &a)
             if (here) {
                 const int l = __ffsll(here) - 1;
                 const int seg = t - (__shfl(upto, l) - __shfl(mine, l)) + (other ? __shfl(used, l) : 0);
-                return Work{(b0 + __builtin_amdgcn_readfirstlane(l)) * a.H + h, __builtin_amdgcn_readfirstlane(seg), false};
+                return Work{(b0 + __builtin_amdgcn_readfirstlane(l)) * a.H + h, __builtin_amdgcn_readfirstlane(seg), false, job};
             }
             t -= __shfl(upto, 63);
         }
     }
-    return Work{0, 0, true};                   // (not reached: the two lists hold every segment)
+    return Work{0, 0, true, 0};                // (not reached: the two lists hold every segment)
 }
 
 // Loads of a chunk of tokens: 16 bytes a lane, 1024 a wave, straight into LDS, the loads of all tiles going round the waves.
 template <typename T>
 struct Loader {
     const ScanArgs &a;
+    int job;
     long long base;          // element offset of the (b,h) slice
     int len, t_end, wave, lane;
     unsigned row_bytes, offset[T::LOADS];
-    __device__ __forceinline__ Loader(const ScanArgs &args, int bh, int length, int end, int w, int l)
-        : a(args), base((long long)tok_base(args.ts, bh, args.H)), len(length), t_end(end), wave(w), lane(l),
+    __device__ __forceinline__ Loader(const ScanArgs &args, int j, int bh, int length, int end, int w, int l)
+        : a(args), job(j), base((long long)tok_base(args.ts, bh, args.H)), len(length), t_end(end), wave(w), lane(l),
           row_bytes((unsigned)args.ts.sn * T::ES)
     {
 #pragma unroll
@@ -295,7 +299,7 @@ struct Loader {
 #pragma unroll
         for (int i = 0; i < T::LOADS; ++i) {
             const int k = i * T::WAVES + wave;
-            const char *src = static_cast<const char *>(a.in[k / T::TILE_LOADS]) + at;
+            const char *src = static_cast<const char *>(a.in[job][k / T::TILE_LOADS]) + at;
             const unsigned off = valid >= 32 ? offset[i] : offset_of(i, valid);
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + off),
                                              (__attribute__((address_space(3))) void *)(set + k * 1024), 16, 0, 0);
@@ -343,7 +347,7 @@ __global__ __launch_bounds__((Scan<DT, D, SUM>::THREADS), 2) void decay_sum_kern
     int chunks = (t_end - t_begin + 31) / 32;
     // What a token adds has 2^-64 of its weight left 64 halvings later, where fp32 sums no longer see it.
     const int first = e2 < 0.f ? max(0, chunks - 1 - (int)fminf(ceilf(-2.f / e2), 0x1p24f)) : 0;
-    const Loader<T> loader(a, work.bh, len, t_end, part, lane);
+    const Loader<T> loader(a, 0, work.bh, len, t_end, part, lane);
     chunks -= first;
     const int t_first = t_begin + 32 * first;
 #pragma unroll
@@ -434,7 +438,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
     const Work work = work_of<T::GROUP>(a);
     if (work.none) return;
     const int seg = work.seg, bh = work.bh, h = bh % a.H;
-    const Role &role = a.role[which];
+    const Role &role = a.role[KIND == DKDV ? which : work.job];
     const bool reverse = a.reverse != 0;
     const int lead = reverse ? 0 : 1;
     const int len = item_length(a.lengths, bh / a.H, a.N);
@@ -449,7 +453,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
                                    q % T::PIECES * 16) = u32x4{0, 0, 0, 0};
     if (seg != 0 && t_begin >= len) return;
 
-    const Loader<T> loader(a, bh, len, t_end, wave, lane);
+    const Loader<T> loader(a, work.job, bh, len, t_end, wave, lane);
     const int chunks = t_begin < t_end ? (t_end - t_begin + 31) / 32 : 0;
 #pragma unroll
     for (int i = 0; i < T::STAGES - 1; ++i)
@@ -798,7 +802,7 @@ struct DecayPlan { int segments, seg_len; };
 DecayPlan decay_plan(const flare_decay_shape &s, bool padded, bool backward)
 {
     // As many segments as keep the scan's waves resident together (two on a SIMD; fp32 from d = 64 on: one).  The backward's
-    // workgroups have waves in two roles: from d = 64 on half as many segments fill the chip.
+    // dK and dV are twice as many waves: from d = 64 on half as many segments fill the chip.
     const long long waves = (s.d < 32 ? 1 : s.d / 32) * (long long)s.B * s.H;
     const long long room = s.d >= 64 && (backward || s.dtype == FLARE_F32) ? 1024 : 2048;
     // A padded batch holds about half of its tokens: twice as many segments, of which as many are empty.
@@ -835,10 +839,11 @@ struct DecayCall {
 ScanArgs scan_args(const DecayCall &c, const DecayPlan &p, const void *in0, const void *in1, const void *in2, const void *in3)
 {
     ScanArgs a{};
-    a.in[0] = in0;
-    a.in[1] = in1;
-    a.in[2] = in2;
-    a.in[3] = in3;
+    a.in[0][0] = in0;
+    a.in[0][1] = in1;
+    a.in[0][2] = in2;
+    a.in[0][3] = in3;
+    a.jobs = 1;
     a.log_decay = c.log_decay;
     a.lengths = c.lengths;
     a.ts = decay_stride(*c.s);
@@ -853,7 +858,7 @@ template <typename T>
 unsigned scan_blocks(const ScanArgs &a)
 {
     const long long round = 8 * T::GROUP;
-    return (unsigned)((a.BH * (long long)a.segments + round - 1) / round * round);
+    return (unsigned)((a.BH * (long long)a.segments + round - 1) / round * round * a.jobs);
 }
 template <int DT, int D, int KIND>
 void launch_scan(const ScanArgs &a, bool exact, int kid, hipStream_t stream)
@@ -935,15 +940,27 @@ struct BackwardPass {
         p = decay_plan(*c.s, c.lengths != nullptr, true);
         split = p.segments > 1;
         if (split) launch_states<DT, D>(c, p, c.q, c.d_o, c.scale, true, c.dstate_out, c.dstate_in, c.slots);
-        a = scan_args(c, p, c.q, c.k, c.v, c.d_o);
+        // x = v, y = dO, z = q and x = k, y = q, z = dO.  d = 128: as two workgroups side by side, which do not wait for each other
+        // (16 heads of 32768 tokens: 195 us, 226 us in one; fp32 8 x 20000: 365, 412).  d < 128: as two roles in one workgroup, which
+        // loads q and dO once (d = 64: 88 us, 110 us in two; fp32 d = 64, 16 x 10007: 98, 125; d = 32, 256 x 4096: 82, 89).
+        const Role dk{c.dk, c.dstate_out, nullptr, 1}, dv{c.dv, c.dstate_out, split ? nullptr : c.dstate_in, 0};
+        if constexpr (D == 128) {
+            a = scan_args(c, p, c.v, c.d_o, c.q, nullptr);
+            a.in[1][0] = c.k;
+            a.in[1][1] = c.q;
+            a.in[1][2] = c.d_o;
+            a.jobs = 2;
+        } else {
+            a = scan_args(c, p, c.q, c.k, c.v, c.d_o);
+        }
         a.slots = split ? c.slots : nullptr;
-        a.role[0] = Role{c.dk, c.dstate_out, nullptr, 1};                                  // x = v, y = dO, z = q
-        a.role[1] = Role{c.dv, c.dstate_out, split ? nullptr : c.dstate_in, 0};            // x = k, y = q, z = dO
+        a.role[0] = dk;
+        a.role[1] = dv;
         a.p = c.scale;
         a.w = 1.f;
         a.m = c.scale;
         a.reverse = 1;
-        launch_scan<DT, D, DKDV>(a, a.role[1].last != nullptr, KID_DECAY_DKDV, c.stream);
+        launch_scan<DT, D, D == 128 ? FORWARD : DKDV>(a, dv.last != nullptr, KID_DECAY_DKDV, c.stream);
         return check_launch();
     }
 };
