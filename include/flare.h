@@ -276,8 +276,9 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
  *     The state goes by the item's own tokens; with none it is handed on unchanged.
  *   - states and their gradients are [B][H][d][d] fp32, rows by q and k, columns by v.
  * 16-bit storage: products of the stored values are exact and sums fp32; <q,k> with its weight, and the state where it
- * meets q, are rounded to the storage type (fp16 behind a common power of two); what is added to the state is not
- * rounded (weights times v to 2^-22 of a term).  f32 storage runs on the fp32 matrix instructions.
+ * meets q, are rounded to the storage type (fp16 behind a common power of two); what is added to a state that is asked
+ * for is good to 2^-22 of a term, otherwise to 2^-16.  A term that the decay has brought below 2^-64 may be left out.  f32
+ * storage runs on the fp32 matrix instructions.
  * With f16 storage scale times q, k, v and d_o must stay below 65504 in magnitude.
  */
 typedef struct {
@@ -307,7 +308,7 @@ int flare_decay_forward(const flare_decay_shape *shape, const void *q, const voi
  *   q, k, v, log_decay, lengths, state_in as in the forward; marks: what it wrote, or NULL                (in)
  *   d_o: o's gradient; dstate_out (or NULL: zero): state_out's                                            (in)
  *   dq, dk, dv: q's shape and dtype; dstate_in (or NULL)                                                  (out)
- * No output may overlap an input.
+ * No output may overlap an input or another output (one buffer for both is refused).
  */
 int flare_decay_backward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
                          const int *lengths, const float *state_in, const float *marks, const void *d_o,
@@ -336,7 +337,8 @@ int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *
  *   - y may be NULL (before the first block): then post and gate are none, and x_out is not written (pass NULL).
  *     pre none: h is not written (pass NULL).
  *   - All arithmetic is fp32; h is formed from x_out before that is rounded.  Outputs are rounded once.
- *   - x_out may be the buffer of x or y, h that of y (not the same as x_out's); dx that of dx_out, dy that of dh or y.
+ *   - x_out may be the buffer of x or y, h that of y (not the same as x_out's); dx that of dx_out, dy that of dh or y.  Two outputs
+ *     in one buffer are refused.
  */
 typedef enum { FLARE_NORM_NONE = 0, FLARE_NORM_LAYER = 1, FLARE_NORM_RMS = 2 } flare_norm;
 typedef enum {

@@ -373,6 +373,13 @@ int flare_decay_backward(const flare_decay_shape *shape, const void *q, const vo
     const int rc = check_decay(shape);
     if (rc != FLARE_OK) return rc;
     if (!q || !k || !v || !log_decay || !d_o || !dq || !dk || !dv) return FLARE_EINVAL;
+    const void *const in[] = {q, k, v, d_o}, *const out[] = {dq, dk, dv};     // whole buffers, at least, are told apart
+    for (int i = 0; i < 3; ++i) {
+        for (const void *t : in)
+            if (out[i] == t) return FLARE_EINVAL;
+        if (out[i] == out[(i + 1) % 3]) return FLARE_EINVAL;
+    }
+    if (dstate_in && (dstate_in == dstate_out || dstate_in == state_in)) return FLARE_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(lengths) ||
         !aligned16(state_in) || !aligned16(marks) || !aligned16(d_o) || !aligned16(dstate_out) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
         !aligned16(dstate_in) || !aligned16(workspace))
@@ -409,6 +416,7 @@ int flare_residual_norm_forward(const flare_norm_shape *shape, const flare_norm_
     const int rc = check_norm_inputs(shape, params, x, y, gate);
     if (rc != FLARE_OK) return rc;
     if ((x_out != nullptr) != (y != nullptr) || (h != nullptr) != (shape->pre != FLARE_NORM_NONE)) return FLARE_EINVAL;
+    if (h && h == x_out) return FLARE_EINVAL;
     if (!aligned16(x_out) || !aligned16(h) || !aligned16(stats)) return FLARE_EALIGN;
     return norm_forward(*shape, params ? *params : flare_norm_params{}, x, y, gate, x_out, h, stats, alpha, eps,
                         static_cast<hipStream_t>(stream));
@@ -425,6 +433,7 @@ int flare_residual_norm_backward(const flare_norm_shape *shape, const flare_norm
     if ((!y && (dx_out || dy || dpost_weight || dpost_bias)) || (shape->gate == FLARE_GATE_NONE && dgate)) return FLARE_EINVAL;
     if (shape->pre == FLARE_NORM_NONE && (dh || dpre_weight || dpre_bias)) return FLARE_EINVAL;
     if (shape->post == FLARE_NORM_NONE && (dpost_weight || dpost_bias)) return FLARE_EINVAL;
+    if ((dx && dx == dy) || (dgate && (dgate == dx || dgate == dy || dgate == gate))) return FLARE_EINVAL;
     if (!aligned16(stats) || !aligned16(dx_out) || !aligned16(dh) || !aligned16(dx) || !aligned16(dy) || !aligned16(dgate) ||
         !aligned16(dpre_weight) || !aligned16(dpre_bias) || !aligned16(dpost_weight) || !aligned16(dpost_bias) ||
         !aligned16(workspace))

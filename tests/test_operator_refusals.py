@@ -8,6 +8,7 @@ from paper_2508_12594_amd import binding
 from paper_2508_12594_amd.binding import DecayShape, FlareError, NormParams, NormShape
 
 P, ODD, ONE = ctypes.c_void_p(4096), ctypes.c_void_p(4100), ctypes.c_float(1)   # never dereferenced: the checks fail first
+A, B, C, S, T = (ctypes.c_void_p(4096 * i) for i in range(2, 7))                # other buffers
 
 
 @pytest.fixture(scope="module")
@@ -38,7 +39,7 @@ def test_decay_arguments(lib):
         a = list(args)
         a[i] = ODD
         assert lib.flare_decay_forward(one, *a, ONE, None, 0, None) == -3
-    back = [P, P, P, P, None, None, None, P, None, P, P, P, None]
+    back = [P, P, P, P, None, None, None, P, None, A, B, C, None]
     for i in (0, 1, 2, 3, 7, 9, 10, 11):
         a = list(back)
         a[i] = None
@@ -47,6 +48,14 @@ def test_decay_arguments(lib):
         a = list(back)
         a[i] = ODD
         assert lib.flare_decay_backward(one, *a, ONE, None, 0, None) == -3
+    for i, other in ((9, P), (10, P), (11, P), (9, B), (10, C), (11, A)):          # an output over an input, over another output
+        a = list(back)
+        a[i] = other
+        assert lib.flare_decay_backward(one, *a, ONE, None, 0, None) == -1
+    for states in ((S, T, S), (T, S, S)):
+        a = list(back)
+        a[5], a[8], a[12] = states
+        assert lib.flare_decay_backward(one, *a, ONE, None, 0, None) == -1
     # a long sequence of few heads is split, and needs its slots
     long = DecayShape(1, 1, 100000, 128, binding.FLARE_BF16, 0)
     f, b, m = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
@@ -98,19 +107,22 @@ def test_norm_arguments(lib):
     assert fwd(norm_shape(pre=0), ctypes.byref(weights), P, P, None, P, None, None, ONE, ONE, None) == -1
     assert fwd(norm_shape(), ctypes.byref(post), P, P, None, P, P, None, ONE, ONE, None) == -1
     assert fwd(norm_shape(), ctypes.byref(crooked), P, P, None, P, P, None, ONE, ONE, None) == -3
+    assert fwd(norm_shape(), None, P, P, None, A, A, None, ONE, ONE, None) == -1                # two outputs in one buffer
     for i in (0, 1, 3, 4, 5):
-        a = [P, P, None, P, P, P]
+        a = [P, P, None, A, B, P]
         a[i] = ODD
         assert fwd(norm_shape(), None, *a, ONE, ONE, None) == -3
     bwd = lib.flare_residual_norm_backward
 
-    def call(shape, x=P, y=P, gate=None, stats=P, dx_out=P, dh=P, dx=P, dy=P, dgate=None, w=(None,) * 4, ws=P, size=1 << 30):
+    def call(shape, x=P, y=P, gate=None, stats=P, dx_out=P, dh=P, dx=P, dy=A, dgate=None, w=(None,) * 4, ws=P, size=1 << 30):
         return bwd(shape, None, x, y, gate, stats, dx_out, dh, dx, dy, dgate, *w, ONE, ws, size, None)
 
     assert call(norm_shape(), x=None) == -1 and call(norm_shape(), stats=None) == -1
     assert call(norm_shape(), y=None) == -1                                                 # gradients of what is not there
     assert call(norm_shape(), dgate=P) == -1 and call(norm_shape(), w=(None, None, P, None)) == -1
     assert call(norm_shape(pre=0), dh=P) == -1 and call(norm_shape(pre=0), dh=None, w=(P, None, None, None)) == -1
+    assert call(norm_shape(), dy=P) == -1 and call(norm_shape(gate=1), gate=B, dgate=A) == -1
+    assert call(norm_shape(gate=1), gate=B, dgate=B) == -1
     assert call(norm_shape(), ws=None) == -4 and call(norm_shape(), size=16) == -4
     assert call(norm_shape(), ws=ODD) == -3 and call(norm_shape(), dy=ODD) == -3 and call(norm_shape(), w=(ODD, None, None, None)) == -3
 
