@@ -104,7 +104,10 @@ struct Scan {
     static constexpr int LOADS = TILES * TILE_LOADS / WAVES;       // and so many of them are each wave's
     // Chunks held in LDS: as many as leave room for eight waves on a CU, at most four (the sums, which have least to do with a
     // chunk; dK and dV).  Scans of three tiles need no more than two: 119 us, 122 with three
-    // (16 heads, 32768 tokens, d = 128).
+    // (16 heads, 32768 tokens, d = 128).  What hides a load is the other waves: the compiler takes an LDS read and a direct load
+    // for possibly the same bytes, and lets a wave wait for all its loads before a chunk's first read.  Stages as arrays of
+    // their own, with the code once for each, take that wait out of every other chunk, and registers with it: 256 x 4096 tokens,
+    // d = 32, 53 -> 52 us; fp32, d = 64, 16 x 10007, 68 -> 64; d = 128 spills, 118 -> 119.  So there is one array.
     static constexpr int FIT = 160 * 1024 / (SET * (WAVES < 8 ? 8 / WAVES : 1));
     static constexpr int STAGES = FIT <= 2 || KIND == FORWARD ? 2 : FIT > 4 ? 4 : FIT;
     static constexpr int STORES = (D < 32 ? 1 : 2) * (ES / 2);   // of a wave, each full chunk
@@ -152,7 +155,10 @@ __device__ __forceinline__ int swizzle(int r)
     else return r >> 3 & 1;
 }
 template <int ROW>
-__device__ __forceinline__ const char *piece_at(const char *tile, int r, int c) { return tile + r * ROW + ((c ^ swizzle<ROW>(r)) << 4); }
+__device__ __forceinline__ const char *piece_at(const char *tile, int r, int c)
+{
+    return tile + r * ROW + ((c ^ swizzle<ROW>(r)) << 4);
+}
 
 // Row `row`, columns 16 s + 8 hh + 0..7
 template <int DT, int D>
@@ -187,7 +193,8 @@ __device__ __forceinline__ Frag<DT> col_frag(const char *tile, int ct, int ks, i
         const int t = 16 * ks + 4 * (lane >> 5);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float x = *reinterpret_cast<const float *>(piece_at<ROW>(tile, t + 8 * (e >> 2) + (e & 3), 8 * ct + (c >> 2)) + 4 * (c & 3));
+            const char *const at = piece_at<ROW>(tile, t + 8 * (e >> 2) + (e & 3), 8 * ct + (c >> 2)) + 4 * (c & 3);
+            const float x = *reinterpret_cast<const float *>(at);
             f.v[e] = D < 32 && (lane & 16) ? 0.f : x;
         }
     } else {
@@ -245,7 +252,7 @@ __device__ __forceinline__ Work work_of(const ScanArgs &a)
     if (work >= a.BH * a.segments) return Work{0, 0, true, 0};
     if (!a.lengths) return Work{work % a.BH, work / a.BH, false, job};
     const int lane = threadIdx.x & 63, items = a.BH / a.H, h = work % a.H;
-    int t = work / a.H;                        // of the segments that hold tokens (the first of an empty item, too), then of the others
+    int t = work / a.H;       // of the segments that hold tokens (the first of an empty item, too), then of the others
     for (int other = 0; other < 2; ++other) {
         for (int b0 = 0; b0 < items; b0 += 64) {
             const int b = b0 + lane;
@@ -465,7 +472,8 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc[ct] = splat16(0.f);
     {
-        const float *s = a.slots ? a.slots + ((size_t)bh * a.segments + seg) * (D * D) : role.first ? role.first + (size_t)bh * (D * D) : nullptr;
+        const float *s = a.slots ? a.slots + ((size_t)bh * a.segments + seg) * (D * D)
+                                 : role.first ? role.first + (size_t)bh * (D * D) : nullptr;
         if (s && col < D) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
@@ -801,17 +809,20 @@ TokStride decay_stride(const flare_decay_shape &s)
 struct DecayPlan { int segments, seg_len; };
 DecayPlan decay_plan(const flare_decay_shape &s, bool padded, bool backward)
 {
-    // As many segments as keep the scan's waves resident together (two on a SIMD; fp32 from d = 64 on: one).  The backward's
-    // dK and dV are twice as many waves: from d = 64 on half as many segments fill the chip.
+    // As many segments as keep the scan's waves resident together (two on a SIMD; fp32 from d = 64 on: one, and at d = 32
+    // the six that a CU's LDS has room for).  The backward's dK and dV are twice as many waves: from d = 64 on, and of fp32
+    // from d = 32 on, half as many segments fill the chip.  (fp32, d = 32: 256 x 2048 tokens forward 110 us, 128 with segments
+    // for eight waves a CU; 64 x 8192 backward 269 us with segments for four, 317 for eight; bf16, 256 x 4096: 210, 205.)
     const long long waves = (s.d < 32 ? 1 : s.d / 32) * (long long)s.B * s.H;
-    const long long room = s.d >= 64 && (backward || s.dtype == FLARE_F32) ? 1024 : 2048;
+    const bool f32 = s.dtype == FLARE_F32;
+    const long long room = f32 && s.d >= 32 ? (backward || s.d >= 64 ? 1024 : 1536) : backward && s.d >= 64 ? 1024 : 2048;
     // A padded batch holds about half of its tokens: twice as many segments, of which as many are empty.
     long long want = (padded ? 2 : 1) * room / waves;
     // Sums and carry cost two launches, about 13 us: as much as 12 chunks one after the other (fp32: 4).  And each segment costs the
     // carry 0.2 us, each chunk of a segment both passes 1.6 us: together least at sqrt(5 N) tokens a segment.  (8 heads of
     // 1000 tokens, d = 64: 36 us in one, 24 us in segments of 256, 18 us of 128.)
     const long long least = (long long)(sqrt(5.0 * s.N) / 32.0 + 0.5) * 32;
-    const long long most = s.N <= (s.dtype == FLARE_F32 ? 128 : 384) ? 1 : (s.N + least - 1) / least;
+    const long long most = s.N <= (f32 ? 128 : 384) ? 1 : (s.N + least - 1) / least;
     if (want > most) want = most;
     if (want < 1) want = 1;
     const long long len = ((s.N + want - 1) / want + 31) / 32 * 32;
