@@ -276,7 +276,8 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
  *     The state goes by the item's own tokens; with none it is handed on unchanged.
  *   - states and their gradients are [B][H][d][d] fp32, rows by q and k, columns by v.
  * 16-bit storage: products of the stored values are exact and sums fp32; <q,k> with its weight, and the state where it
- * meets q, are rounded to the storage type (fp16 behind a common power of two); what is added to a state that is asked
+ * meets q, are each taken as the sum of two numbers of the storage type, good to 2^-16 (bf16) or 2^-22 (fp16, behind a
+ * common power of two), so that an output is as good as rounded once; what is added to a state that is asked
  * for is good to 2^-22 of a term, otherwise to 2^-16.  A term that the decay has brought below 2^-64 may be left out.  f32
  * storage runs on the fp32 matrix instructions.
  * With f16 storage scale times q, k, v and d_o must stay below 65504 in magnitude.

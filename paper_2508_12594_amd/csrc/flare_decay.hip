@@ -12,7 +12,7 @@
 // its matrix accumulators (fp32) from the first token of its segment to the last.  Per 32 tokens, with the layouts of
 // v_mfma_f32_32x32x16 (flare_mfma_common.h):
 //   P^T = Y X^T            lane = token of x, registers = tokens of y; weighted by l^(t-u) (0 above the diagonal)
-//   O^T = C^T X^T          the state's accumulators, rounded, are the A operand as they lie
+//   O^T = C^T X^T          the state's accumulators, as two numbers of 16 bits, are the A operand as they lie
 //   O^T += Z^T P^T         likewise P^T's accumulators are the B operand: a contraction index in accumulator order
 //   C   += Y^T (weight Z)  Y and Z read down their columns (transposing LDS reads), Y's columns in the order that makes the
 //                          state's registers eight neighbouring rows (state_row)
@@ -284,20 +284,27 @@ struct Loader {
     int job;
     long long base;          // element offset of the (b,h) slice
     int len, t_end, wave, lane;
-    unsigned row_bytes, offset[T::LOADS];
+    // (of a wave's loads, those of a tile lie like those of the next where the loads of a tile go evenly round the waves)
+    static constexpr int OFFSETS = T::TILE_LOADS % T::WAVES == 0 ? T::TILE_LOADS / T::WAVES : T::LOADS;
+    unsigned row_bytes, offset[OFFSETS];
     __device__ __forceinline__ Loader(const ScanArgs &args, int j, int bh, int length, int end, int w, int l)
         : a(args), job(j), base((long long)tok_base(args.ts, bh, args.H)), len(length), t_end(end), wave(w), lane(l),
           row_bytes((unsigned)args.ts.sn * T::ES)
     {
 #pragma unroll
-        for (int i = 0; i < T::LOADS; ++i) offset[i] = offset_of(i, 32);
+        for (int i = 0; i < OFFSETS; ++i) {
+            const int q = place(i), r = q / T::PIECES, c = (q % T::PIECES) ^ swizzle<T::ROW>(r);
+            offset[i] = (unsigned)(a.reverse ? 31 - r : r) * row_bytes + 16 * c;
+        }
     }
+    __device__ __forceinline__ int place(int i) const { return (i * T::WAVES + wave) % T::TILE_LOADS * 64 + lane; }
     // of load i, from the chunk's first row in memory
     __device__ __forceinline__ unsigned offset_of(int i, int valid) const
     {
-        const int q = (i * T::WAVES + wave) % T::TILE_LOADS * 64 + lane, r = q / T::PIECES;
-        const int c = (q % T::PIECES) ^ swizzle<T::ROW>(r), rc = min(r, valid - 1);   // behind the end: the last row again
-        return (unsigned)(a.reverse ? 31 - rc : rc) * row_bytes + 16 * c;
+        const unsigned off = offset[i % OFFSETS];
+        if (valid >= 32) return off;
+        const unsigned back = (unsigned)max(place(i) / T::PIECES - valid + 1, 0) * row_bytes;    // behind the end: the last row again
+        return a.reverse ? off + back : off - back;
     }
     __device__ __forceinline__ void load(int t0, char *set) const
     {
@@ -307,8 +314,7 @@ struct Loader {
         for (int i = 0; i < T::LOADS; ++i) {
             const int k = i * T::WAVES + wave;
             const char *src = static_cast<const char *>(a.in[job][k / T::TILE_LOADS]) + at;
-            const unsigned off = valid >= 32 ? offset[i] : offset_of(i, valid);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + off),
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + offset_of(i, valid)),
                                              (__attribute__((address_space(3))) void *)(set + k * 1024), 16, 0, 0);
         }
     }
@@ -332,6 +338,11 @@ __device__ __forceinline__ void split_planes(const float *x, Frag<DT> (&plane)[P
 }
 template <int DT, bool EXACT>
 constexpr int planes() { return DT == FLARE_F32 ? 1 : DT == FLARE_BF16 && EXACT ? 3 : 2; }
+// ... of the weighted scores and of the state where it meets x: one alone would add as much to an output's error as the rounding of
+// the output itself (bf16 2.3e-3 of the norm, 1.7e-3 with two).  The second costs 2 ... 4 % of a pass (16 heads of 131072 tokens, d = 128,
+// forward 673 -> 687 us; 32 x 8 x 4096, d = 32, with its gradients 251 -> 258 us; 333 tokens of 8 heads 16.3 -> 19.1 us).
+template <int DT>
+constexpr int operand_planes() { return DT == FLARE_F32 ? 1 : 2; }
 
 // A segment's own sum, into its slot: sum_u l^(n-u-lead) y_u z_u^T.  From the segment's last chunk to its first, so that its
 // first tokens are the last to be read before the scan reads them again (256 MB of memory-side cache), and nothing has to be
@@ -437,7 +448,7 @@ template <int DT, int D, int KIND, bool EXACT>
 __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::PER_SIMD)) void decay_scan_kernel(const ScanArgs a)
 {
     using T = Scan<DT, D, KIND>;
-    constexpr int STEPS = D / 16, CT = T::CT, PLANES = planes<DT, EXACT>();
+    constexpr int STEPS = D / 16, CT = T::CT, PLANES = planes<DT, EXACT>(), OPERAND = operand_planes<DT>();
     constexpr bool F16 = DT == FLARE_F16;
     __shared__ __align__(1024) char lds[T::STAGES * T::SET];
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
@@ -530,7 +541,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
     };
     fit_state();
     // One chunk.  PLAIN: of 32 tokens, and slow decays.  The weighted z goes in planes: what the state sums is then good to 2^-22
-    // (fp16) or 2^-24 (bf16) of a term; a state that is no output only meets x rounded to 16 bits, and 2^-16 will do with bf16.
+    // (fp16) or 2^-24 (bf16) of a term; a state that is no output only goes into results of 16 bits, and 2^-16 will do with bf16.
     const auto chunk = [&](auto plain_tag, int t0, const char *set) {
         constexpr bool PLAIN = decltype(plain_tag)::value;
         const char *const tx = set + x_at, *const ty = set + y_at, *const tz = set + z_at;
@@ -551,7 +562,10 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
                 float c8[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) c8[e] = F16 ? acc[s >> 1][8 * (s & 1) + e] * down_state : acc[s >> 1][8 * (s & 1) + e];
-                o = mma<DT>(pack8<DT>(c8), xf, o);
+                Frag<DT> plane[OPERAND];
+                split_planes<DT, OPERAND>(c8, plane);
+#pragma unroll
+                for (int k = 0; k < OPERAND; ++k) o = mma<DT>(plane[k], xf, o);
             }
             float p16[16];
 #pragma unroll
@@ -570,10 +584,10 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
             for (int r = 0; r < 16; ++r) o[r] *= scale_o;
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                float p8[8];
+                Frag<DT> plane[OPERAND];
+                split_planes<DT, OPERAND>(p16 + 8 * ks, plane);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p8[e] = p16[8 * ks + e];
-                o = mma<DT>(zc[ks], pack8<DT>(p8), o);
+                for (int k = 0; k < OPERAND; ++k) o = mma<DT>(zc[ks], plane[k], o);
             }
             const int t = t0 + l32;
             char *const row = static_cast<char *>(role.out) +
@@ -681,13 +695,16 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
     }
 
     float *const dst = role.last ? role.last + (size_t)bh * (D * D) : nullptr;
-    if (dst && col < D) {
+    int here = lane;
+    asm volatile("" : "+v"(here));      // (addresses formed anew, not kept over the chunks)
+    const int to = 32 * part + (here & 31);
+    if (dst && to < D) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int row = state_row(ct, r, hh);
-                if (D >= 32 || row < D) dst[(size_t)row * D + col] = F16 ? ldexpf(acc[ct][r], e_z) : acc[ct][r];
+                const int row = state_row(ct, r, here >> 5);
+                if (D >= 32 || row < D) dst[(size_t)row * D + to] = F16 ? ldexpf(acc[ct][r], e_z) : acc[ct][r];
             }
     }
 }
