@@ -320,6 +320,7 @@ int flare_decay_backward(const flare_decay_shape *shape, const void *q, const vo
  * One token of each item: shape->N is 1 (else FLARE_EINVAL); q, k, v, o are [B][H][d].
  *   active [B] int32 or NULL: an item with active[b] <= 0 has no token now: its state is handed on, its o is zero  (in)
  *   state_in, state_out: may be one buffer                                                            (in, out)
+ * o may be the buffer of q, k or v.
  */
 int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
                      const int *active, const float *state_in, float *state_out, void *o, float scale, void *stream);

@@ -1020,7 +1020,10 @@ int run_step(const flare_decay_shape &s, const void *q, const void *k, const voi
     const int BH = s.B * s.H;
     constexpr int NARROW = D < 32 ? D : 32;
     LaunchTimer timer(KID_DECAY_STEP, stream);
-    if (D > 32 && BH >= 512)
+    // The blocks of a state all read the whole of q and k: o may lie over those only where one workgroup has them all (it reads them
+    // before its barrier, and writes o behind it).
+    const bool over = o == q || o == k;
+    if (D > 32 && (BH >= 512 || over))
         decay_step_kernel<DT, D, D><<<BH, 256, 0, stream>>>(q, k, v, log_decay, active, state_in, state_out, o, scale, s.H);
     else
         decay_step_kernel<DT, D, NARROW><<<BH * (D / NARROW), 256, 0, stream>>>(q, k, v, log_decay, active, state_in, state_out, o,
