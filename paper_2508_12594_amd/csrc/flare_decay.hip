@@ -120,6 +120,13 @@ struct Scan {
 __device__ __forceinline__ float decay_log2(float g) { return g <= 0.f ? fmaxf(g * kLog2e, -3000.f) : __builtin_nanf(""); }
 __device__ __forceinline__ int item_length(const int *lengths, int b, int N) { return lengths ? min(max(lengths[b], 0), N) : N; }
 
+// A value that is the same in all lanes, in a scalar register
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+// l^n
+__device__ __forceinline__ double exact_decay(float g, int n)
+{
+    return g <= 0.f ? exp(fmax((double)g, -2080.0) * n) : (double)__builtin_nanf("");
+}
 // l^n for a factor that is applied again and again: the two fp32 numbers around it, of which `next` gives the one that takes
 // the product of all factors so far back towards the exact power.  (One of them alone is off by up to 2^-25, always the same
 // way: 2^-18 after a hundred chunks.)
@@ -127,7 +134,7 @@ struct Fade {
     float up, down, err_up, err_down, drift;
     __device__ __forceinline__ Fade(float g, int n)
     {
-        const double exact = g <= 0.f ? exp(fmax((double)g, -2080.0) * n) : (double)__builtin_nanf("");
+        const double exact = exact_decay(g, n);
         up = down = (float)exact;
         if ((double)up < exact) up = __uint_as_float(__float_as_uint(up) + 1);
         else if ((double)down > exact) down = __uint_as_float(__float_as_uint(down) - 1);
@@ -513,6 +520,9 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
     };
     update_weights(32);
     Fade fade(g, 32);
+    // of the last chunk, if that is a part of one, as two numbers: calls of a few tokens each apply the same one over and over
+    const double part_exact = exact_decay(g, max(t_end - t_begin, 0) % 32);
+    const float part_faded = uniform((float)part_exact), part_rest = uniform((float)(part_exact - (double)(float)part_exact));
     // The accumulators hold C / (f 2^e_z).  With slow decays f takes up the decay of the chunks, and is multiplied in where it has
     // become small; otherwise (a chunk leaves less than 2^-16) the accumulators themselves are multiplied in each chunk.
     float f = 1.f;
@@ -546,10 +556,12 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
         constexpr bool PLAIN = decltype(plain_tag)::value;
         const char *const tx = set + x_at, *const ty = set + y_at, *const tz = set + z_at;
         __builtin_amdgcn_s_setprio(1);       // (the waves of a SIMD then are less often in the same part)
-        float faded = fade.next();
-        if (!PLAIN && t0 + 32 > t_end) {
+        float faded = fade.next(), rest = 0.f;
+        const bool partial = !PLAIN && t0 + 32 > t_end;
+        if (partial) {
             update_weights(t_end - t0);
-            faded = fast_exp2(e2 * (t_end - t0));
+            faded = part_faded;
+            rest = part_rest;
         }
 
         const Frag<DT> zc[2] = {col_frag<DT, D, false>(tz, part, 0, lane), col_frag<DT, D, false>(tz, part, 1, lane)};
@@ -640,7 +652,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[ct][r] *= faded;
+                for (int r = 0; r < 16; ++r) acc[ct][r] = partial ? fmaf(acc[ct][r], faded, acc[ct][r] * rest) : acc[ct][r] * faded;
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
@@ -791,14 +803,17 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const void *q, const vo
     float vc[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < 4; ++e) vc[e] = load_elem<DT>(v, row + c0 + c + e);
-    const float fade = fast_exp2(decay_log2(log_decay[bh % H]));
+    // l as two fp32 numbers: one alone is off by up to 2^-25, in every step the same way (16384 steps: 5e-4 of the oldest terms);
+    // with both a step rounds its result and nothing else.
+    const double exact = exact_decay(log_decay[bh % H], 1);
+    const float fade = (float)exact, rest = (float)(exact - (double)fade);
+    const auto next = [&](float old, float kr, float vc) { return fmaf(kr, vc, fmaf(old, fade, old * rest)); };
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const int r = g + i * GROUPS;
         if (r < D) {
             float4 t = s[i];
-            if (on) t = make_float4(fmaf(kr[i], vc[0], fade * t.x), fmaf(kr[i], vc[1], fade * t.y), fmaf(kr[i], vc[2], fade * t.z),
-                                    fmaf(kr[i], vc[3], fade * t.w));
+            if (on) t = make_float4(next(t.x, kr[i], vc[0]), next(t.y, kr[i], vc[1]), next(t.z, kr[i], vc[2]), next(t.w, kr[i], vc[3]));
             *reinterpret_cast<float4 *>(state_out + at + (size_t)r * D) = t;
             acc[0] = fmaf(qr[i], t.x, acc[0]);
             acc[1] = fmaf(qr[i], t.y, acc[1]);
