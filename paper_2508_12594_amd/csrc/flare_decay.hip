@@ -228,9 +228,20 @@ __device__ __forceinline__ int exponent_step(float largest, int e)
     if (e > -96 && !__any(largest > 4.f) && __any(largest > 0.f)) return -kExponentStep;
     return 0;
 }
-// Scales v until it is fit; returns the factor it took.
 template <int N>
-__device__ __forceinline__ float fit_exponent(float (&v)[N], int &e)
+__device__ __forceinline__ float largest_of(const f32x16 (&v)[N])
+{
+    float largest = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(v[i][r]));
+    return largest;
+}
+// Scales v until it is fit, or until what it is added to (whose largest magnitude, before that, is `held`) would come near the end of
+// fp32 (what is lost then is 2^-80 of that); returns the factor it took.
+template <int N, typename Held>
+__device__ __forceinline__ float fit_exponent(float (&v)[N], int &e, const Held &held)
 {
     float took = 1.f;
     for (;;) {
@@ -238,7 +249,7 @@ __device__ __forceinline__ float fit_exponent(float (&v)[N], int &e)
 #pragma unroll
         for (int r = 0; r < N; ++r) largest = fmaxf(largest, fabsf(v[r]));
         const int step = exponent_step(largest, e);
-        if (step == 0) return took;
+        if (step == 0 || (step < 0 && __any(held() * took > 0x1p84f))) return took;
         e += step;
         const float by = step > 0 ? 1.f / (1 << kExponentStep) : (float)(1 << kExponentStep);
         took *= by;
@@ -410,7 +421,7 @@ __global__ __launch_bounds__((Scan<DT, D, SUM>::THREADS), 2) void decay_sum_kern
 #pragma unroll
         for (int r = 0; r < 16; ++r) weighted[r] = elem_of<DT>(zc[r >> 3], r & 7) * (wu[r] * (behind * down_z));
         if constexpr (F16) {
-            const float took = fit_exponent(weighted, e_z);
+            const float took = fit_exponent(weighted, e_z, [&]() { return largest_of(acc); });
             if (took != 1.f) {
                 down_z *= took;
 #pragma unroll
@@ -536,11 +547,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
 
     const auto fit_state = [&]() {
         if constexpr (F16) {
-            float largest = 0.f;
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(acc[ct][r]));
+            const float largest = largest_of(acc);
             for (;;) {
                 const int step = exponent_step(largest * down_state, e_state);
                 if (step == 0) break;
@@ -584,7 +591,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
             for (int r = 0; r < 16; ++r) p16[r] = p[r] * wp[r];
             float scale_o = wi * f, scale_out = 1.f;
             if constexpr (F16) {
-                const float took = fit_exponent(p16, e_p);
+                const float took = fit_exponent(p16, e_p, []() { return 0.f; });
                 if (took != 1.f) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) wp[r] *= took;
@@ -639,7 +646,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
 #pragma unroll
         for (int r = 0; r < 16; ++r) weighted[r] = elem_of<DT>(zc[r >> 3], r & 7) * (PLAIN || F16 ? wu[r] * lift : wu[r]);
         if constexpr (F16) {
-            const float took = fit_exponent(weighted, e_z);
+            const float took = fit_exponent(weighted, e_z, [&]() { return largest_of(acc); });
             if (took != 1.f) {
                 down_z *= took;
 #pragma unroll
