@@ -280,7 +280,8 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
  * common power of two), so that an output is as good as rounded once; what is added to a state that is asked
  * for is good to 2^-22 of a term, otherwise to 2^-16.  A term that the decay has brought below 2^-64 may be left out.  f32
  * storage runs on the fp32 matrix instructions.
- * With f16 storage scale times q, k, v and d_o must stay below 65504 in magnitude.
+ * With f16 storage scale times q, k, v and d_o must stay below 65504 in magnitude; with bf16 and f32 states, their
+ * gradients, and those times rows of q, k, v or d_o below 1e33.
  */
 typedef struct {
     int B, H, N, d;

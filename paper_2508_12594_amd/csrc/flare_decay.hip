@@ -535,7 +535,8 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
     const double part_exact = exact_decay(g, max(t_end - t_begin, 0) % 32);
     const float part_faded = uniform((float)part_exact), part_rest = uniform((float)(part_exact - (double)(float)part_exact));
     // The accumulators hold C / (f 2^e_z).  With slow decays f takes up the decay of the chunks, and is multiplied in where it has
-    // become small; otherwise (a chunk leaves less than 2^-16) the accumulators themselves are multiplied in each chunk.
+    // become small, so that it is never below 2^-16; otherwise (a chunk leaves less than that) the accumulators themselves are
+    // multiplied in each chunk.
     float f = 1.f;
     // fp16: exponents of the weighted z, of P (in wp too) and of the state as an operand
     int e_z = 0, e_p = 0, e_state = 0;
@@ -703,7 +704,7 @@ __global__ __launch_bounds__((Scan<DT, D, KIND>::THREADS), (Scan<DT, D, KIND>::P
         const int full = t_begin < t_end ? (t_end - t_begin) / 32 : 0;
         for (; i < full; ++i) {
             const char *const set = next_chunk();
-            if (f < kSlow) take_up();
+            if (f * fade.down < kSlow) take_up();
             chunk(PlainTag<true>{}, t_begin + 32 * i, set);
         }
         take_up();

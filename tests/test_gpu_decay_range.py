@@ -42,3 +42,16 @@ def test_fp16_small_terms_behind_a_large_sum(large_first):
     for n in ("q", "k", "v", "d_o"):
         wide[n] = dev[n].double().cpu()
     run(dev, wide, 1.0, "f16", N, d)
+
+
+@pytest.mark.parametrize("dtype,N", [("f32", 120), ("bf16", 300), ("bf16", 700)])
+def test_large_states_of_wide_types(dtype, N):
+    """Values of 1e31: what a slow decay leaves is kept as a factor beside the state, which must not leave fp32 for that.  (The first
+    two sequences are not cut into segments.)"""
+    d = 32
+    decays = [-halvings * math.log(2.0) / 32 for halvings in (15.9, 9.0, 7.9, 3.0)]
+    print("[case] 1e31 %s" % dtype, flush=True)
+    dev, wide = make(1, 4, N, d, dtype, 7, decays=decays)
+    dev["v"] = dev["v"] * 1e31
+    wide["v"] = dev["v"].double().cpu()
+    run(dev, wide, 0.1, dtype, N, d)
