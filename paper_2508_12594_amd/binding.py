@@ -318,7 +318,10 @@ def decay_backward(q, k, v, log_decay, d_o, scale, lengths=None, state=None, dst
 
 def decay_step(q, k, v, log_decay, state, scale, state_out=None, active=None, o=None, stream=None):
     """flare_decay_step: one token of each item, q, k, v [B,H,d]; returns o [B,H,d].  state [B,H,d,d] fp32 is advanced in
-    place, or into state_out.  active [B] int32: items with 0 are left out (their state stays, their o is zero)."""
+    place, or into state_out.  active [B] int32: items with 0 are left out (their state stays, their o is zero).
+
+    As after any operation in place, a backward pass that had saved the tensor (decay_mixer saves `state`) then raises: for a
+    state that is still to be differentiated pass state_out."""
     return (_ext or _native()).decay_step(q, k, v, log_decay, state, scale, state_out, active, o, stream)
 
 

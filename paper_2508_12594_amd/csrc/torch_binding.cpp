@@ -487,6 +487,14 @@ OptTensor defined(const Tensor &t) { return t.defined() ? OptTensor(t) : std::nu
 // a part of a Tensor list that may be missing
 OptTensor contiguous(const OptTensor &t) { return t ? OptTensor(t->contiguous()) : std::nullopt; }
 
+// Tensors of the caller's that a call has written: autograd has to know, or a backward pass that had saved one would go on with its
+// new values.
+void written(std::initializer_list<const OptTensor *> outputs)
+{
+    for (const OptTensor *t : outputs)
+        if (*t && !(*t)->is_inference()) (*t)->unsafeGetTensorImpl()->bump_version();
+}
+
 // A backward pass that is captured into a graph must not meet a leaf whose gradient accumulator an eager graph still holds
 // on another stream: the engine would make the two streams wait for each other, which ends the capture and the process.
 void check_capture(std::initializer_list<const OptTensor *> inputs)
@@ -598,6 +606,7 @@ std::tuple<Tensor, OptTensor> decay_forward(const Tensor &q, const Tensor &k, co
                             dev(o, "o", dt, q.sizes()), f32(dev(so, "state_out", at::kFloat, dim.state)),
                             f32(marks_ptr(marks, need.marks)), (float)scale, ws.ptr, ws.bytes, to.stream),
           "flare_decay_forward");
+    written({&o_in, &state_out_in, &marks});
     return {o, so};
 }
 
@@ -628,6 +637,7 @@ std::tuple<Tensor, Tensor, Tensor, OptTensor> decay_backward(const Tensor &q, co
                              dev(dq, "dq", dt, q.sizes()), dev(dk, "dk", dt, q.sizes()), dev(dv, "dv", dt, q.sizes()),
                              f32(dev(ds, "dstate_in", at::kFloat, dim.state)), (float)scale, ws.ptr, ws.bytes, to.stream),
           "flare_decay_backward");
+    written({&dq_in, &dk_in, &dv_in, &dstate_in});
     return {dq, dk, dv, ds};
 }
 
@@ -654,6 +664,7 @@ Tensor decay_step(const Tensor &q, const Tensor &k, const Tensor &v, const Tenso
                          cf32(dev(state, "state", at::kFloat, dim.state)), f32(dev(so, "state_out", at::kFloat, dim.state)),
                          dev(o, "o", dt, q.sizes()), (float)scale, to.stream),
           "flare_decay_step");
+    written({state_out ? &state_out : &os, &o_in});
     return o;
 }
 
@@ -849,6 +860,7 @@ std::tuple<OptTensor, OptTensor> norm_forward(const Tensor &x, const OptTensor &
                            dev(x_out, "x_out", x.scalar_type(), x.sizes()), dev(h, "h", dt, x.sizes()),
                            f32(dev(stats, "stats", at::kFloat, stats_dim(s))), (float)alpha, (float)eps, to.stream),
           "flare_residual_norm_forward");
+    written({&x_out_in, &h_in, &stats});
     return {x_out, h};
 }
 
