@@ -340,8 +340,8 @@ int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *
  *   - y may be NULL (before the first block): then post and gate are none, and x_out is not written (pass NULL).
  *     pre none: h is not written (pass NULL).
  *   - All arithmetic is fp32; h is formed from x_out before that is rounded.  Outputs are rounded once.
- *   - x_out may be the buffer of x or y, h that of y (not the same as x_out's); dx that of dx_out, dy that of dh or y.  Two outputs
- *     in one buffer are refused.
+ *   - x_out may be the buffer of x, h that of y, dx that of x or dx_out, dy that of y or dh; without x_f32, where all rows have one
+ *     size, also x_out that of y, h that of x, dx that of y or dh, dy that of x or dx_out.  Two outputs in one buffer are refused.
  */
 typedef enum { FLARE_NORM_NONE = 0, FLARE_NORM_LAYER = 1, FLARE_NORM_RMS = 2 } flare_norm;
 typedef enum {

@@ -417,6 +417,7 @@ int flare_residual_norm_forward(const flare_norm_shape *shape, const flare_norm_
     if (rc != FLARE_OK) return rc;
     if ((x_out != nullptr) != (y != nullptr) || (h != nullptr) != (shape->pre != FLARE_NORM_NONE)) return FLARE_EINVAL;
     if (h && h == x_out) return FLARE_EINVAL;
+    if (shape->x_f32 && ((x_out && x_out == y) || (h && h == x))) return FLARE_EINVAL;    // (rows of another size)
     if (!aligned16(x_out) || !aligned16(h) || !aligned16(stats)) return FLARE_EALIGN;
     return norm_forward(*shape, params ? *params : flare_norm_params{}, x, y, gate, x_out, h, stats, alpha, eps,
                         static_cast<hipStream_t>(stream));
