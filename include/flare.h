@@ -298,7 +298,7 @@ int flare_decay_workspace_bytes(const flare_decay_shape *shape, int padded, size
  *   q, k, v, log_decay, lengths (or NULL), state_in (or NULL: zero)                                       (in)
  *   o: q's shape and dtype; state_out (or NULL)                                                           (out)
  *   marks (or NULL): states along the sequences, which save the backward a pass over k and v             (out)
- * o may be the buffer of q, k or v, and state_out that of state_in.
+ * o may be the buffer of q, k or v, and state_out that of state_in; any other overlap of an output is refused.
  */
 int flare_decay_forward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
                         const int *lengths, const float *state_in, void *o, float *state_out, float *marks, float scale,
@@ -310,7 +310,7 @@ int flare_decay_forward(const flare_decay_shape *shape, const void *q, const voi
  *   q, k, v, log_decay, lengths, state_in as in the forward; marks: what it wrote, or NULL                (in)
  *   d_o: o's gradient; dstate_out (or NULL: zero): state_out's                                            (in)
  *   dq, dk, dv: q's shape and dtype; dstate_in (or NULL)                                                  (out)
- * No output may overlap an input or another output (one buffer for both is refused).
+ * No output may overlap an input or another output (refused).
  */
 int flare_decay_backward(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
                          const int *lengths, const float *state_in, const float *marks, const void *d_o,
@@ -321,7 +321,7 @@ int flare_decay_backward(const flare_decay_shape *shape, const void *q, const vo
  * One token of each item: shape->N is 1 (else FLARE_EINVAL); q, k, v, o are [B][H][d].
  *   active [B] int32 or NULL: an item with active[b] <= 0 has no token now: its state is handed on, its o is zero  (in)
  *   state_in, state_out: may be one buffer                                                            (in, out)
- * o may be the buffer of q, k or v.
+ * o may be the buffer of q, k or v; any other overlap of an output is refused.
  */
 int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
                      const int *active, const float *state_in, float *state_out, void *o, float scale, void *stream);
@@ -341,7 +341,7 @@ int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *
  *     pre none: h is not written (pass NULL).
  *   - All arithmetic is fp32; h is formed from x_out before that is rounded.  Outputs are rounded once.
  *   - x_out may be the buffer of x, h that of y, dx that of x or dx_out, dy that of y or dh; without x_f32, where all rows have one
- *     size, also x_out that of y, h that of x, dx that of y or dh, dy that of x or dx_out.  Two outputs in one buffer are refused.
+ *     size, also x_out that of y, h that of x, dx that of y or dh, dy that of x or dx_out.  Any other overlap of an output is refused.
  */
 typedef enum { FLARE_NORM_NONE = 0, FLARE_NORM_LAYER = 1, FLARE_NORM_RMS = 2 } flare_norm;
 typedef enum {

@@ -98,6 +98,42 @@ int check_shape(const flare_shape *s)
     return FLARE_OK;
 }
 
+// A buffer of a call.  An output may lie over an input of its own kind, if it is exactly that buffer (kind 0: over none): every
+// element is then read by the lane, or before the barrier, that writes it.
+struct Buffer {
+    const void *at;
+    size_t bytes;
+    int kind;
+};
+bool overlap(const Buffer &a, const Buffer &b)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return x && y && x < y + b.bytes && y < x + a.bytes;
+}
+template <int OUTS, int INS>
+int check_buffers(const Buffer (&out)[OUTS], const Buffer (&in)[INS])
+{
+    for (int i = 0; i < OUTS; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return FLARE_EINVAL;
+        for (const Buffer &b : in)
+            if (overlap(out[i], b) && !(out[i].kind != 0 && out[i].kind == b.kind && out[i].at == b.at && out[i].bytes == b.bytes))
+                return FLARE_EINVAL;
+    }
+    return FLARE_OK;
+}
+enum { FIXED = 0, ROWS = 1, STATES = 2 };
+
+// Bytes of the decay mixer's buffers
+struct DecaySizes {
+    size_t rows, states, heads, items;
+    explicit DecaySizes(const flare_decay_shape &s)
+        : rows((size_t)s.B * s.H * s.N * s.d * (s.dtype == FLARE_F32 ? 4 : 2)), states((size_t)s.B * s.H * s.d * s.d * 4),
+          heads((size_t)s.H * 4), items((size_t)s.B * 4)
+    {
+    }
+};
+
 int check_decay(const flare_decay_shape *s)
 {
     if (!s) return FLARE_EINVAL;
@@ -124,6 +160,17 @@ int check_norm(const flare_norm_shape *s)
     if (s->C > 8192 || s->rows >= (1LL << 31)) return FLARE_EUNSUPPORTED;
     return FLARE_OK;
 }
+
+// Bytes of its buffers.  (A gate that rows share is smaller than they are.)
+struct NormSizes {
+    size_t x, rows, gate, stats, params;
+    explicit NormSizes(const flare_norm_shape &s)
+        : rows((size_t)s.rows * s.C * (s.dtype == FLARE_F32 ? 4 : 2)), stats((size_t)s.rows * 16), params((size_t)s.C * 4)
+    {
+        x = s.x_f32 ? (size_t)s.rows * s.C * 4 : rows;
+        gate = s.gate == FLARE_GATE_NONE ? 0 : rows / (size_t)s.rows_per_gate;
+    }
+};
 
 // What both directions of the residual norm ask of their inputs.
 int check_norm_inputs(const flare_norm_shape *s, const flare_norm_params *p, const void *x, const void *y, const void *gate)
@@ -362,6 +409,12 @@ int flare_decay_forward(const flare_decay_shape *shape, const void *q, const voi
         return FLARE_EALIGN;
     const size_t need = decay_fwd_bytes(*shape, lengths != nullptr, marks != nullptr);
     if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
+    const DecaySizes n(*shape);
+    const Buffer out[] = {{o, n.rows, ROWS}, {state_out, n.states, STATES}, {marks, decay_marks_bytes(*shape, lengths != nullptr), FIXED},
+                          {workspace, need, FIXED}};
+    const Buffer in[] = {{q, n.rows, ROWS}, {k, n.rows, ROWS}, {v, n.rows, ROWS}, {log_decay, n.heads, FIXED}, {lengths, n.items, FIXED},
+                         {state_in, n.states, STATES}};
+    if (check_buffers(out, in) != FLARE_OK) return FLARE_EINVAL;
     return decay_forward(*shape, q, k, v, log_decay, lengths, state_in, o, state_out, marks, scale, workspace,
                          static_cast<hipStream_t>(stream));
 }
@@ -386,6 +439,13 @@ int flare_decay_backward(const flare_decay_shape *shape, const void *q, const vo
         return FLARE_EALIGN;
     const size_t need = decay_bwd_bytes(*shape, lengths != nullptr, marks != nullptr);
     if (need != 0 && (!workspace || workspace_bytes < need)) return FLARE_EWORKSPACE;
+    const DecaySizes n(*shape);
+    const Buffer outs[] = {{dq, n.rows, FIXED}, {dk, n.rows, FIXED}, {dv, n.rows, FIXED}, {dstate_in, n.states, FIXED},
+                           {workspace, need, FIXED}};
+    const Buffer ins[] = {{q, n.rows, ROWS}, {k, n.rows, ROWS}, {v, n.rows, ROWS}, {d_o, n.rows, ROWS}, {log_decay, n.heads, FIXED},
+                          {lengths, n.items, FIXED}, {state_in, n.states, STATES}, {dstate_out, n.states, STATES},
+                          {marks, decay_marks_bytes(*shape, lengths != nullptr), FIXED}};
+    if (check_buffers(outs, ins) != FLARE_OK) return FLARE_EINVAL;
     return decay_backward(*shape, q, k, v, log_decay, lengths, state_in, marks, d_o, dstate_out, dq, dk, dv, dstate_in, scale, workspace,
                           static_cast<hipStream_t>(stream));
 }
@@ -399,6 +459,11 @@ int flare_decay_step(const flare_decay_shape *shape, const void *q, const void *
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(log_decay) || !aligned16(active) || !aligned16(state_in) ||
         !aligned16(state_out) || !aligned16(o))
         return FLARE_EALIGN;
+    const DecaySizes n(*shape);
+    const Buffer out[] = {{o, n.rows, ROWS}, {state_out, n.states, STATES}};
+    const Buffer in[] = {{q, n.rows, ROWS}, {k, n.rows, ROWS}, {v, n.rows, ROWS}, {log_decay, n.heads, FIXED}, {active, n.items, FIXED},
+                         {state_in, n.states, STATES}};
+    if (check_buffers(out, in) != FLARE_OK) return FLARE_EINVAL;
     return decay_step(*shape, q, k, v, log_decay, active, state_in, state_out, o, scale, static_cast<hipStream_t>(stream));
 }
 
@@ -417,9 +482,14 @@ int flare_residual_norm_forward(const flare_norm_shape *shape, const flare_norm_
     if (rc != FLARE_OK) return rc;
     if ((x_out != nullptr) != (y != nullptr) || (h != nullptr) != (shape->pre != FLARE_NORM_NONE)) return FLARE_EINVAL;
     if (h && h == x_out) return FLARE_EINVAL;
-    if (shape->x_f32 && ((x_out && x_out == y) || (h && h == x))) return FLARE_EINVAL;    // (rows of another size)
     if (!aligned16(x_out) || !aligned16(h) || !aligned16(stats)) return FLARE_EALIGN;
-    return norm_forward(*shape, params ? *params : flare_norm_params{}, x, y, gate, x_out, h, stats, alpha, eps,
+    const NormSizes n(*shape);
+    const flare_norm_params p = params ? *params : flare_norm_params{};
+    const Buffer out[] = {{x_out, n.x, ROWS}, {h, n.rows, ROWS}, {stats, n.stats, FIXED}};
+    const Buffer in[] = {{x, n.x, ROWS}, {y, n.rows, ROWS}, {gate, n.gate, ROWS}, {p.pre_weight, n.params, FIXED},
+                         {p.pre_bias, n.params, FIXED}, {p.post_weight, n.params, FIXED}, {p.post_bias, n.params, FIXED}};
+    if (check_buffers(out, in) != FLARE_OK) return FLARE_EINVAL;
+    return norm_forward(*shape, p, x, y, gate, x_out, h, stats, alpha, eps,
                         static_cast<hipStream_t>(stream));
 }
 
@@ -440,7 +510,16 @@ int flare_residual_norm_backward(const flare_norm_shape *shape, const flare_norm
         !aligned16(workspace))
         return FLARE_EALIGN;
     if (!workspace || workspace_bytes < norm_bwd_bytes(*shape)) return FLARE_EWORKSPACE;
-    return norm_backward(*shape, params ? *params : flare_norm_params{}, x, y, gate, stats, dx_out, dh, dx, dy, dgate, dpre_weight,
+    const NormSizes n(*shape);
+    const flare_norm_params p = params ? *params : flare_norm_params{};
+    const Buffer out[] = {{dx, n.x, ROWS}, {dy, n.rows, ROWS}, {dgate, n.gate, ROWS}, {dpre_weight, n.params, FIXED},
+                          {dpre_bias, n.params, FIXED}, {dpost_weight, n.params, FIXED}, {dpost_bias, n.params, FIXED},
+                          {workspace, norm_bwd_bytes(*shape), FIXED}};
+    const Buffer in[] = {{x, n.x, ROWS}, {y, n.rows, ROWS}, {gate, n.gate, FIXED}, {stats, n.stats, FIXED}, {dx_out, n.x, ROWS},
+                         {dh, n.rows, ROWS}, {p.pre_weight, n.params, FIXED}, {p.pre_bias, n.params, FIXED},
+                         {p.post_weight, n.params, FIXED}, {p.post_bias, n.params, FIXED}};
+    if (check_buffers(out, in) != FLARE_OK) return FLARE_EINVAL;
+    return norm_backward(*shape, p, x, y, gate, stats, dx_out, dh, dx, dy, dgate, dpre_weight,
                          dpre_bias, dpost_weight, dpost_bias, alpha, workspace, static_cast<hipStream_t>(stream));
 }
 

@@ -27,3 +27,21 @@ def test_step_writes_over_its_inputs(B, H, d, dtype):
         assert o is mine[i] and torch.equal(state, want_state), "qkv"[i]
         # (two roundings that may go different ways, by a half step each)
         assert ((o.double() - want.double()).abs() <= tol * size + 2 * u * want.double().abs() + 2.0 ** -24).all(), "qkv"[i]
+
+
+@pytest.mark.parametrize("d,dtype,N,layout", [(128, "bf16", 1500, "bnhd"), (32, "f32", 200, "bhnd")])
+def test_sequences_write_over_their_inputs(d, dtype, N, layout):
+    """o over k and over v too, the state over the one that came in; a buffer that only begins at the same place is refused."""
+    print("[case] sequences over their inputs d%d %s N%d %s" % (d, dtype, N, layout), flush=True)
+    dev, _ = make(1, 3, N, d, dtype, 47, layout, state=True)
+    names = ("q", "k", "v")
+    want, want_state = binding.decay_forward(*(dev[n] for n in names), dev["log_decay"], 0.2, state=dev["state"], want_state=True,
+                                             layout=layout)
+    for i in range(3):
+        mine, state = [dev[n].clone() for n in names], dev["state"].clone()
+        o, _ = binding.decay_forward(*mine, dev["log_decay"], 0.2, state=state, state_out=state, o=mine[i], layout=layout)
+        assert o is mine[i] and torch.equal(o, want) and torch.equal(state, want_state), names[i]
+    room = torch.empty(dev["q"].numel() + 64, dtype=dev["q"].dtype, device="cuda")
+    q, shifted = room[:-64].view_as(dev["q"]), room[64:].view_as(dev["q"])
+    with pytest.raises(binding.FlareError):
+        binding.decay_forward(q, dev["k"], dev["v"], dev["log_decay"], 0.2, o=shifted, layout=layout)
