@@ -367,7 +367,8 @@ __global__ __launch_bounds__(Lanes<LPR>::THREADS) void residual_norm_backward_ke
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float sg = sigmoid(g[i]), rest = 1.f - sg;
+                        // 1 - sigmoid from the exponential where it is small (the difference has no bits left at g = 17)
+                        const float t = fast_exp2(-kLog2e * g[i]), sg = __builtin_amdgcn_rcpf(1.f + t), rest = g[i] > 0.f ? t * sg : 1.f - sg;
                         act[i] = a.act == FLARE_GATE_SIGMOID ? sg : g[i] * sg;
                         g[i] = a.act == FLARE_GATE_SIGMOID ? sg * rest : sg * fmaf(g[i], rest, 1.f);
                     }
