@@ -268,7 +268,8 @@ __device__ __forceinline__ Work work_of(const ScanArgs &a)
     const int job = a.jobs == 2 ? blockIdx.x >> 3 & 1 : 0, turn = blockIdx.x >> (a.jobs == 2 ? 4 : 3);
     const int work = (turn / GROUP * 8 + (blockIdx.x & 7)) * GROUP + turn % GROUP;
     if (work >= a.BH * a.segments) return Work{0, 0, true, 0};
-    if (!a.lengths) return Work{work % a.BH, work / a.BH, false, job};
+    // (with one segment each there is nothing to look for; with more (b,h) are few)
+    if (!a.lengths || a.segments == 1) return Work{work % a.BH, work / a.BH, false, job};
     const int lane = threadIdx.x & 63, items = a.BH / a.H, h = work % a.H;
     int t = work / a.H;       // of the segments that hold tokens (the first of an empty item, too), then of the others
     for (int other = 0; other < 2; ++other) {
