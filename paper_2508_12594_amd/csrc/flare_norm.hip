@@ -532,9 +532,10 @@ NormPlan norm_plan(const flare_norm_shape &s)
     const int lanes = row_lanes(s.C), slots = row_slots(lanes);
     const bool shared = s.gate != FLARE_GATE_NONE && s.rows_per_gate > 1;
     const long long group_rows = shared ? s.rows_per_gate : s.rows, groups = s.rows / group_rows;
-    // as many workgroups as are on the chip together (two or three waves a SIMD), of at least four rounds of rows
+    // as many workgroups as are on the chip together (two or three waves a SIMD), of at least four rounds of rows (of which rows that
+    // share a gate have their own)
     const long long most = lanes <= 256 ? 768 : lanes == 512 ? 512 : 256;
-    long long want = s.rows / (4LL * slots);
+    long long want = groups * ((group_rows + slots - 1) / slots) / 4;
     want = want < 1 ? 1 : want > most ? most : want;
     p.units_per_group = groups >= want ? 1 : (want + groups - 1) / groups;
     long long rows = (group_rows + p.units_per_group - 1) / p.units_per_group;
