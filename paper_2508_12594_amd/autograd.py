@@ -51,6 +51,32 @@ def flare_mixer(q_lat, k, v, scale, layout="bhnd", y_f32=False):
     return y
 
 
+_ONCE = None
+
+
+def _once(of, grads, inputs):
+    """Gradients that a graph is asked of are constants to it: a derivative of them, which would be lost without a word, raises."""
+    import torch
+    global _ONCE
+    if not torch.is_grad_enabled():
+        return grads
+    if _ONCE is None:
+        class Once(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, of, count, *tensors):
+                ctx.of = of
+                return tuple(t.view_as(t) for t in tensors[:count])
+
+            @staticmethod
+            def backward(ctx, *_):
+                raise binding.FlareError(ctx.of + " has no second derivative")
+
+        _ONCE = Once
+    there = [g for g in grads if g is not None]
+    made = iter(_ONCE.apply(of, len(there), *there, *(t for t in inputs if t is not None)))
+    return tuple(None if g is None else next(made) for g in grads)
+
+
 _RECORDED_DECAY = None
 
 
@@ -77,6 +103,7 @@ def _recorded_decay():
                     q, k, v, log_decay, d_o.contiguous(), ctx.scale, lengths=lengths, state=state,
                     dstate_out=None if dstate_out is None else dstate_out.contiguous(),
                     want_dstate=state is not None and ctx.needs_input_grad[5], layout=ctx.layout)
+                dq, dk, dv, dstate = _once("decay_mixer", (dq, dk, dv, dstate), (q, k, v, state, d_o, dstate_out))
                 return dq, dk, dv, None, None, dstate, None, None, None
 
         _RECORDED_DECAY = RecordedDecayMixer
@@ -87,7 +114,7 @@ def decay_mixer(q, k, v, log_decay, scale, lengths=None, state=None, want_state=
     """Causal linear attention with a decay for each head (flare_decay_forward): per head S_t = exp(log_decay) S_{t-1} + k_t v_t^T,
     o_t = scale S_t^T q_t.  q, k, v [B,H,N,d] ('bhnd') or [B,N,H,d] ('bnhd'), log_decay [H] fp32 and at most 0 (a constant: it is
     not differentiated), lengths [B] int32 for a padded batch, state [B,H,d,d] fp32 from an earlier piece of the
-    sequences.  Returns (o, state_out), state_out None without want_state.  Differentiable in q, k, v and state."""
+    sequences.  Returns (o, state_out), state_out None without want_state.  Differentiable in q, k, v and state (once)."""
     out = binding._native().decay_mixer(q, k, v, log_decay, float(scale), lengths, state, bool(want_state),
                                         binding._layout(layout))
     if out is None:
@@ -126,8 +153,8 @@ def _recorded_norm():
                 dh = grads.pop(0) if ctx.outputs[1] else None
                 stats, x, y, gate, *params = ctx.saved_tensors
                 names = ("pre_weight", "pre_bias", "post_weight", "post_bias")
-                return binding.residual_norm_backward(x, y, dx_out, dh, stats, gate=gate, **dict(zip(names, params)),
-                                                      **ctx.kinds) + (None, None, None)
+                out = binding.residual_norm_backward(x, y, dx_out, dh, stats, gate=gate, **dict(zip(names, params)), **ctx.kinds)
+                return _once("residual_norm", out, [x, y, gate, dx_out, dh] + params) + (None, None, None)
 
         _RECORDED_NORM = RecordedResidualNorm
     return _RECORDED_NORM
@@ -137,7 +164,7 @@ def residual_norm(x, y=None, gate=None, pre="layer", post="none", pre_weight=Non
                   gate_act="none", alpha=1.0, eps=1e-5, h_dtype=None):
     """x_out = x + alpha * post(y) * gate_act(gate) and h = pre(x_out) in one pass (flare_residual_norm_forward; shapes as in
     binding.residual_norm_forward).  Returns (x_out, h): without y x_out is x, with pre 'none' h is None.  Differentiable in
-    all tensors."""
+    all tensors (once)."""
     kinds = dict(pre=pre, post=post, gate_act=gate_act, alpha=float(alpha))
     out = binding._native().residual_norm(x, y, gate, binding._norm(pre, "pre"), binding._norm(post, "post"), binding._gate(gate_act),
                                           pre_weight, pre_bias, post_weight, post_bias, float(alpha), float(eps), h_dtype)

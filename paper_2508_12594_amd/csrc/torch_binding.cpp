@@ -535,6 +535,29 @@ torch::autograd::variable_list raising(const F &f)
     }
 }
 
+// Gradients that a graph is asked of (create_graph) are constants to it: a derivative of them would be lost without a word.
+struct NoSecondDerivative : torch::autograd::Node {
+    std::string of;
+    std::string name() const override { return "FlareNoSecondDerivative"; }
+    torch::autograd::variable_list apply(torch::autograd::variable_list &&) override
+    {
+        return raising([&]() -> torch::autograd::variable_list { throw Error(of + " has no second derivative"); });
+    }
+};
+// `node`: whose gradients these are.  The history leads to all that they depend on, so that a backward pass to any of it comes by.
+void no_second_derivative(torch::autograd::Node &node, const char *of, const torch::autograd::variable_list &grads_in,
+                          torch::autograd::variable_list &grads)
+{
+    if (!at::GradMode::is_enabled()) return;
+    auto raises = std::shared_ptr<NoSecondDerivative>(new NoSecondDerivative(), torch::autograd::deleteNode);
+    raises->of = of;
+    torch::autograd::edge_list to = node.next_edges();
+    for (torch::autograd::Edge &e : torch::autograd::collect_next_edges(grads_in)) to.push_back(std::move(e));
+    raises->set_next_edges(std::move(to));
+    for (Tensor &t : grads)
+        if (t.defined()) torch::autograd::set_history(t, raises);
+}
+
 struct DecayDims {
     std::array<int64_t, 4> state;
     std::array<int64_t, 1> heads, items;
@@ -683,7 +706,11 @@ struct DecayBackward : torch::autograd::Node {
     torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override
     {
         std::lock_guard<std::mutex> lock(mutex_);
-        return raising([&] { return gradients(std::move(grads[0]), grads.size() > 1 ? std::move(grads[1]) : Tensor()); });
+        return raising([&] {
+            auto out = gradients(Tensor(grads[0]), grads.size() > 1 ? Tensor(grads[1]) : Tensor());
+            no_second_derivative(*this, "decay_mixer", grads, out);
+            return out;
+        });
     }
     torch::autograd::variable_list gradients(Tensor &&d_o, Tensor &&dstate)
     {
@@ -926,9 +953,13 @@ struct NormBackward : torch::autograd::Node {
     torch::autograd::variable_list apply(torch::autograd::variable_list &&grads) override
     {
         std::lock_guard<std::mutex> lock(mutex_);
-        return raising([&] { return gradients(std::move(grads)); });
+        return raising([&] {
+            auto out = gradients(grads);
+            no_second_derivative(*this, "residual_norm", grads, out);
+            return out;
+        });
     }
-    torch::autograd::variable_list gradients(torch::autograd::variable_list &&grads)
+    torch::autograd::variable_list gradients(const torch::autograd::variable_list &grads)
     {
         // (the outputs are x_out, if there is a y, and h, if there is a pre norm)
         OptTensor dx_out = has_y ? contiguous(defined(grads[0])) : std::nullopt,
