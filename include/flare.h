@@ -278,8 +278,8 @@ int flare_spectral(const flare_shape *shape, const void *q_lat, const void *k, c
  * 16-bit storage: products of the stored values are exact and sums fp32; <q,k> with its weight, and the state where it
  * meets q, are each taken as the sum of two numbers of the storage type, good to 2^-16 (bf16) or 2^-22 (fp16, behind a
  * common power of two), so that an output is as good as rounded once; what is added to a state that is asked
- * for is good to 2^-22 of a term, otherwise to 2^-16.  A term that the decay has brought below 2^-64 may be left out.  f32
- * storage runs on the fp32 matrix instructions.
+ * for is good to 2^-22 of a term, otherwise to 2^-16.  A term that the decay has brought below 2^-64 may be left out, and with
+ * f16 one below 2^-80 of the state's largest entry.  f32 storage runs on the fp32 matrix instructions.
  * With f16 storage scale times q, k, v and d_o must stay below 65504 in magnitude; with bf16 and f32 states, their
  * gradients, and those times rows of q, k, v or d_o below 1e33.
  */

@@ -108,7 +108,7 @@ struct Buffer {
 bool overlap(const Buffer &a, const Buffer &b)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-    return x && y && x < y + b.bytes && y < x + a.bytes;
+    return x && y && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
 }
 template <int OUTS, int INS>
 int check_buffers(const Buffer (&out)[OUTS], const Buffer (&in)[INS])

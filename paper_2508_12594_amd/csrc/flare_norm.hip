@@ -534,10 +534,10 @@ NormPlan norm_plan(const flare_norm_shape &s)
     const int lanes = row_lanes(s.C), slots = row_slots(lanes);
     const bool shared = s.gate != FLARE_GATE_NONE && s.rows_per_gate > 1;
     const long long group_rows = shared ? s.rows_per_gate : s.rows, groups = s.rows / group_rows;
-    // as many workgroups as are on the chip together (two or three waves a SIMD), of at least four rounds of rows (of which rows that
-    // share a gate have their own)
+    // as many workgroups as are on the chip together (two or three waves a SIMD), of at least four rounds of rows; rows that share a
+    // gate have their own rounds (128 rows of 128 channels, a gate for every two: 14.5 us, 98 us with full rounds counted)
     const long long most = lanes <= 256 ? 768 : lanes == 512 ? 512 : 256;
-    long long want = groups * ((group_rows + slots - 1) / slots) / 4;
+    long long want = (shared ? groups * ((group_rows + slots - 1) / slots) : s.rows / slots) / 4;
     want = want < 1 ? 1 : want > most ? most : want;
     p.units_per_group = groups >= want ? 1 : (want + groups - 1) / groups;
     long long rows = (group_rows + p.units_per_group - 1) / p.units_per_group;
