@@ -103,11 +103,12 @@ struct Scan {
     static constexpr int TILE_LOADS = BYTES / 1024;                // wave-wide loads of a tile; those of all tiles go round the waves
     static constexpr int LOADS = TILES * TILE_LOADS / WAVES;       // and so many of them are each wave's
     // Chunks held in LDS: as many as leave room for eight waves on a CU, at most four (the sums, which have least to do with a
-    // chunk; dK and dV).  Scans of three tiles need no more than two: 119 us, 122 with three
-    // (16 heads, 32768 tokens, d = 128).  What hides a load is the other waves: the compiler takes an LDS read and a direct load
+    // chunk; dK and dV).  Scans of three tiles need no more than two: 127 us, 142 with three
+    // (16 heads, 32768 tokens, d = 128, bf16).  What hides a load is the other waves: the compiler takes an LDS read and a direct load
     // for possibly the same bytes, and lets a wave wait for all its loads before a chunk's first read.  Stages as arrays of
-    // their own, with the code once for each, take that wait out of every other chunk, and registers with it: 256 x 4096 tokens,
-    // d = 32, 53 -> 52 us; fp32, d = 64, 16 x 10007, 68 -> 64; d = 128 spills, 118 -> 119.  So there is one array.
+    // their own, with the code once for each, take that wait out of every other chunk, and registers with it (with operands of one
+    // number): 256 x 4096 tokens, d = 32, 53 -> 52 us; fp32, d = 64, 16 x 10007, 68 -> 64; d = 128 spills, 118 -> 119.  So there is
+    // one array.
     static constexpr int FIT = 160 * 1024 / (SET * (WAVES < 8 ? 8 / WAVES : 1));
     static constexpr int STAGES = FIT <= 2 || KIND == FORWARD ? 2 : FIT > 4 ? 4 : FIT;
     static constexpr int STORES = (D < 32 ? 1 : 2) * (ES / 2);   // of a wave, each full chunk
@@ -260,7 +261,8 @@ __device__ __forceinline__ float fit_exponent(float (&v)[N], int &e, const Held 
 
 // Which (b,h) and segment a workgroup has.  Workgroups go round the eight XCDs: neighbouring heads whose rows share lines
 // (with [B][N][H][d]) go to one.  In a padded batch the segments that hold tokens come first, or the workgroups that have
-// anything to do would share some CUs and leave others empty (8 items of 0 to 4097 tokens, 16 heads: 151 us, 87 us like this).
+// anything to do would share some CUs and leave others empty (8 items of 0 to 4097 tokens, 16 heads, d = 128, fp16: sums and scan
+// 201 us, 161 us like this).
 struct Work { int bh, seg; bool none; int job; };
 template <int GROUP>
 __device__ __forceinline__ Work work_of(const ScanArgs &a)
@@ -358,8 +360,9 @@ __device__ __forceinline__ void split_planes(const float *x, Frag<DT> (&plane)[P
 template <int DT, bool EXACT>
 constexpr int planes() { return DT == FLARE_F32 ? 1 : DT == FLARE_BF16 && EXACT ? 3 : 2; }
 // ... of the weighted scores and of the state where it meets x: one alone would add as much to an output's error as the rounding of
-// the output itself (bf16 2.3e-3 of the norm, 1.7e-3 with two).  The second costs 2 ... 4 % of a pass (16 heads of 131072 tokens, d = 128,
-// forward 673 -> 687 us; 32 x 8 x 4096, d = 32, with its gradients 251 -> 258 us; 333 tokens of 8 heads 16.3 -> 19.1 us).
+// the output itself (bf16 2.3e-3 of the norm, 1.7e-3 with two).  The second costs 1 ... 5 % of a pass (16 heads of 131072 tokens, d = 128,
+// forward 674 -> 682 us; 32 x 8 x 4096, d = 32, with its gradients 251 -> 259 us; 16 x 32768, d = 128, 639 -> 672 us), and 333 tokens of
+// 8 heads, one chunk after the other, take 19.6 us for 16.4.
 template <int DT>
 constexpr int operand_planes() { return DT == FLARE_F32 ? 1 : 2; }
 
@@ -853,15 +856,16 @@ DecayPlan decay_plan(const flare_decay_shape &s, bool padded, bool backward)
     // As many segments as keep the scan's waves resident together (two on a SIMD; fp32 from d = 64 on: one, and at d = 32
     // the six that a CU's LDS has room for).  The backward's dK and dV are twice as many waves: from d = 64 on, and of fp32
     // from d = 32 on, half as many segments fill the chip.  (fp32, d = 32: 256 x 2048 tokens forward 110 us, 128 with segments
-    // for eight waves a CU; 64 x 8192 backward 269 us with segments for four, 317 for eight; bf16, 256 x 4096: 210, 205.)
+    // for eight waves a CU; 64 x 8192 backward 269 us with segments for four, 317 for eight; bf16, 256 x 4096, the backward's sums, dK
+    // and dV: 138, 131.)
     const long long waves = (s.d < 32 ? 1 : s.d / 32) * (long long)s.B * s.H;
     const bool f32 = s.dtype == FLARE_F32;
     const long long room = f32 && s.d >= 32 ? (backward || s.d >= 64 ? 1024 : 1536) : backward && s.d >= 64 ? 1024 : 2048;
     // A padded batch holds about half of its tokens: twice as many segments, of which as many are empty.
     long long want = (padded ? 2 : 1) * room / waves;
-    // Sums and carry cost two launches, about 13 us: as much as 12 chunks one after the other (fp32: 4).  And each segment costs the
-    // carry 0.2 us, each chunk of a segment both passes 1.6 us: together least at sqrt(5 N) tokens a segment.  (8 heads of
-    // 1000 tokens, d = 64: 36 us in one, 24 us in segments of 256, 18 us of 128.)
+    // Sums and carry cost two launches, about 13 us: as much as 9 to 12 chunks one after the other (fp32: 4).  And each segment costs
+    // the carry 0.2 us, each chunk of a segment both passes 1.6 us and more: together least at about sqrt(5 N) tokens a segment.
+    // (8 heads of 1000 tokens, d = 64, bf16, kernel times: 48 us in one, 34 us in segments of 256, 24 us in the 64 that this gives.)
     const long long least = (long long)(sqrt(5.0 * s.N) / 32.0 + 0.5) * 32;
     const long long most = s.N <= (f32 ? 128 : 384) ? 1 : (s.N + least - 1) / least;
     if (want > most) want = most;
@@ -993,8 +997,8 @@ struct BackwardPass {
         split = p.segments > 1;
         if (split) launch_states<DT, D>(c, p, c.q, c.d_o, c.scale, true, c.dstate_out, c.dstate_in, c.slots);
         // x = v, y = dO, z = q and x = k, y = q, z = dO.  d = 128: as two workgroups side by side, which do not wait for each other
-        // (16 heads of 32768 tokens: 195 us, 226 us in one; fp32 8 x 20000: 365, 412).  d < 128: as two roles in one workgroup, which
-        // loads q and dO once (d = 64: 88 us, 110 us in two; fp32 d = 64, 16 x 10007: 98, 125; d = 32, 256 x 4096: 82, 89).
+        // (16 heads of 32768 tokens: 226 us, 278 us in one; fp32 8 x 20000: 354, 342).  d < 128: as two roles in one workgroup, which
+        // loads q and dO once (d = 64: 99 us, 109 us in two; fp32 d = 64, 16 x 10007: 89, 115; d = 32, 256 x 4096: 97, 107).
         const Role dk{c.dk, c.dstate_out, nullptr, 1}, dv{c.dv, c.dstate_out, split ? nullptr : c.dstate_in, 0};
         if constexpr (D == 128) {
             a = scan_args(c, p, c.v, c.d_o, c.q, nullptr);
