@@ -1,4 +1,4 @@
-"""The new nodes have first derivatives: a second one raises, rather than come out without their part."""
+"""The decay mixer and the residual norm have first derivatives: a second one raises, rather than come out without their part."""
 import pytest
 import torch
 
